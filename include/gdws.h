@@ -314,6 +314,86 @@ GDWS_API gdws_status_t gdws_forward_static(gdws_plan_t *plan, const gdws_tensor_
 GDWS_API size_t gdws_static_scratch_bytes(void);
 
 /*
+ * Rows in 8 bits.  What the PW stage sums over is a row: the channels of one pixel of an NHWC map (z of gdws_depthwise, too), or
+ * the features of one token.  The calls below hold rows as 8-bit integers with one fp32 scale each -- half the bytes of bf16 and
+ * twice its tensor-core rate -- and run the pointwise product on them.  (No counterpart in the paper, whose networks are fp32.)
+ * They need no plan, keep nothing between calls, allocate nothing and may be captured into graphs; calls from several host
+ * threads at once are independent.  Buffers are those of the current device.
+ *
+ * Element (r, c) of gdws_rows_t is ptr[r * ld + c], of gdws_rows8_t it stands for scale[r] * q[r * ld + c].  rows >= 0 (at most
+ * 2^31 - 1; with 0 rows nothing is done and pointers may be NULL), cols >= 1, ld >= cols (not looked at for a single row).
+ * Pointers need the alignment of their element type only, whatever the general rule says.  Nothing but the elements themselves is
+ * read or written: neither what lies between cols and ld nor rows behind the last one.  Outputs must not overlap inputs or each
+ * other except where noted; columns of one buffer that do not meet (same ld) are no overlap.
+ */
+typedef struct {
+    void *ptr; /* DEVICE */
+    int64_t rows, ld;
+    int cols;
+    gdws_dtype_t dtype;
+} gdws_rows_t;
+typedef struct {
+    int8_t *q;    /* DEVICE, see above                      */
+    float *scale; /* DEVICE, `rows` entries, one behind the other */
+    int64_t rows, ld;
+    int cols;
+} gdws_rows8_t;
+
+/*
+ * gdws_quantize_rows -- each row of x in 8 bits:  m = max_c |x[r,c]|,  q[r,c] = 127 x[r,c] / m rounded to the nearest integer (to
+ * the even one of two as near; exactly: the quotient is not rounded first),  scale[r] = m / 127.  -128 does not occur.  A row of
+ * zeros gets scale 0.  A row that holds an infinity or a NaN gets scale NaN and zeros, so that everything computed from it is NaN.
+ *   x   F32 or BF16;  q   same rows and cols, written
+ * Also what brings weights [D][G] (a row is what one output channel multiplies) into the form of gdws_pointwise8.
+ * Errors: GDWS_ERR_INVALID_ARG, GDWS_ERR_ARCH, GDWS_ERR_CUDA.
+ */
+GDWS_API gdws_status_t gdws_quantize_rows(const gdws_rows_t *x, const gdws_rows8_t *q, void *stream);
+
+/*
+ * gdws_norm_quantize_rows -- residual addition, root-mean-square norm over the row and 8 bits in one pass:
+ *     h = x + residual,   total = h,   q, scale = 8 bits of  h[c] * weight[c] / sqrt(mean_c h[c]^2 + eps)
+ * h and u = h * weight are fp32; total is h rounded to its type, but the norm and q are those of h before that.  The norm, one
+ * number a row, goes into the scale only: q = round(127 u / max |u|) as in gdws_quantize_rows, whatever the norm.
+ *   residual   NULL: none;  total   NULL: not written.  Type, rows and cols of x.  total may be the very rows of x or of residual
+ *   weight     DEVICE, cols entries of weight_dtype (F32 or BF16), NULL: ones
+ *   eps        finite, at least 2^-126
+ * Sums are fp32.  A row with an infinity or NaN in x, residual, h * weight or the sum of squares gets scale NaN and zeros.
+ * Errors: as gdws_quantize_rows.
+ */
+GDWS_API gdws_status_t gdws_norm_quantize_rows(const gdws_rows_t *x, const gdws_rows_t *residual, const gdws_rows_t *total,
+                                               const void *weight, gdws_dtype_t weight_dtype, float eps, const gdws_rows8_t *q,
+                                               void *stream);
+
+/* gdws_dequantize_rows -- y[r,c] = scale[r] * q[r,c] in fp32, rounded to y's type: rows for the calls that take bf16 or fp32. */
+GDWS_API gdws_status_t gdws_dequantize_rows(const gdws_rows8_t *q, const gdws_rows_t *y, void *stream);
+
+/*
+ * gdws_pointwise8 -- the pointwise product on rows in 8 bits:
+ *     y[r,d] = (sum_c x.q[r,c] * w.q[d,c]) * w.scale[d] * x.scale[r] + bias[d],      relu != 0: negative values become 0
+ *   x      rows of activations;  w   D rows of weights (w->rows = D >= 1, w->cols = x->cols), a scale for each output channel
+ *   bias   DEVICE float[D] or NULL;  y   F32 or BF16, x->rows x D, written
+ * The sums are exact (32-bit integers; cols <= 131071, else GDWS_ERR_UNSUPPORTED), then fp32 in the order written, the last
+ * multiplication and the bias as one fused multiply-add, and one rounding to y's type.  NaN stays NaN through the ReLU.
+ * Rows of x and w that start at multiples of 16 bytes (pointer and ld) run on the tensor cores, others on the ALUs.
+ * Errors: as gdws_quantize_rows, GDWS_ERR_UNSUPPORTED.
+ */
+GDWS_API gdws_status_t gdws_pointwise8(const gdws_rows8_t *x, const gdws_rows8_t *w, const float *bias, int relu,
+                                       const gdws_rows_t *y, void *stream);
+
+/* The kernels of gdws_pointwise8. */
+typedef enum {
+    GDWS_KERNEL8_ALU = 1 /* any alignment */
+} gdws_kernel8_t;
+/* gdws_pointwise8_kernel -- the kernel that this call takes on the current device (a B200 where there is none).  Diagnostic, host only. */
+GDWS_API gdws_status_t gdws_pointwise8_kernel(const gdws_rows8_t *x, const gdws_rows8_t *w, const gdws_rows_t *y, int *kernel);
+
+/*
+ * gdws_rows_status -- as gdws_status, for the calls on rows: reads and clears the status word that those on the current device
+ * share; synchronises with the device.
+ */
+GDWS_API gdws_status_t gdws_rows_status(void);
+
+/*
  * gdws_status -- read (and clear) the plan's device status word; synchronises with the
  * device.  GDWS_OK, or GDWS_ERR_DEVICE_TIMEOUT if a bounded wait inside a kernel expired
  * (the kernel then skipped its remaining work; outputs of that launch are undefined).

@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import os
 import struct
+import threading
 from typing import Optional, Sequence, Tuple
 
 import numpy as np
@@ -25,6 +26,7 @@ OPT_PATH, OPT_RELU, OPT_TILE, OPT_A_LAYOUT, OPT_DW_MATH, OPT_OUT_DTYPE = range(6
 PATH_AUTO, PATH_FUSED, PATH_UNFUSED = 0, 1, 2
 (KERNEL_TWO_STAGES_ALU, KERNEL_TWO_STAGES_TC, KERNEL_FOLDED_PAIRS, KERNEL_FOLDED_SLICES, KERNEL_F32_ALU, KERNEL_F32_PIECES,
  KERNEL_GDW_ALU, KERNEL_GDW_TC) = range(1, 9)
+KERNEL8_ALU, = range(1, 2)
 
 EXPORTS = [
     "gdws_plan", "gdws_plan_set_option", "gdws_plan_info", "gdws_plan_tables", "gdws_plan_tile",
@@ -32,7 +34,8 @@ EXPORTS = [
     "gdws_depthwise", "gdws_pointwise", "gdws_forward_host", "gdws_status", "gdws_launch_count",
     "gdws_last_error", "gdws_version", "gdws_destroy", "gdws_forward_static", "gdws_static_scratch_bytes",
     "gdws_measure_fma_rate", "gdws_measure_code_size", "gdws_selftest_wait", "gdws_plan_gdw_stage", "gdws_plan_form",
-    "gdws_plan_kernel",
+    "gdws_plan_kernel", "gdws_quantize_rows", "gdws_norm_quantize_rows", "gdws_dequantize_rows", "gdws_pointwise8",
+    "gdws_pointwise8_kernel", "gdws_rows_status",
 ]
 
 
@@ -50,6 +53,19 @@ class Tensor(ctypes.Structure):
 
 _PACK_TENSOR = struct.Struct("@P6i").pack_into      # the fields of gdws_tensor_t in one call
 assert struct.calcsize("@P6i") == ctypes.sizeof(Tensor)
+
+class Rows(ctypes.Structure):
+    """Mirror of gdws_rows_t."""
+    _fields_ = [("ptr", ctypes.c_void_p), ("rows", ctypes.c_int64), ("ld", ctypes.c_int64), ("cols", ctypes.c_int), ("dtype", ctypes.c_int)]
+
+
+class Rows8(ctypes.Structure):
+    """Mirror of gdws_rows8_t."""
+    _fields_ = [("q", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("rows", ctypes.c_int64), ("ld", ctypes.c_int64), ("cols", ctypes.c_int)]
+
+
+_PACK_ROWS, _PACK_ROWS8 = struct.Struct("@Pqqii"), struct.Struct("@PPqqi4x")
+assert _PACK_ROWS.size == ctypes.sizeof(Rows) and _PACK_ROWS8.size == ctypes.sizeof(Rows8)
 
 _lib = None
 
@@ -114,6 +130,18 @@ def lib() -> ctypes.CDLL:
     L.gdws_selftest_wait.restype = ci
     L.gdws_launch_count.argtypes = [vp]
     L.gdws_launch_count.restype = i64
+    L.gdws_quantize_rows.argtypes = [vp, vp, vp]
+    L.gdws_quantize_rows.restype = ci
+    L.gdws_norm_quantize_rows.argtypes = [vp, vp, vp, vp, ci, ctypes.c_float, vp, vp]
+    L.gdws_norm_quantize_rows.restype = ci
+    L.gdws_dequantize_rows.argtypes = [vp, vp, vp]
+    L.gdws_dequantize_rows.restype = ci
+    L.gdws_pointwise8.argtypes = [vp, vp, vp, ci, vp, vp]
+    L.gdws_pointwise8.restype = ci
+    L.gdws_pointwise8_kernel.argtypes = [vp, vp, vp, pint]
+    L.gdws_pointwise8_kernel.restype = ci
+    L.gdws_rows_status.argtypes = []
+    L.gdws_rows_status.restype = ci
     L.gdws_last_error.argtypes = []
     L.gdws_last_error.restype = ctypes.c_char_p
     L.gdws_version.argtypes = []
@@ -344,3 +372,133 @@ class Plan:
     def selftest_wait(self, polls: int = 64, stream=None) -> None:
         """gdws_selftest_wait: a bounded wait that runs out; the next status() raises GDWS_ERR_DEVICE_TIMEOUT once."""
         _check(lib().gdws_selftest_wait(self._h, polls, _stream(stream)))
+
+
+# ---- rows in 8 bits
+
+class _Descriptors(threading.local):
+    """Descriptors of one call, filled anew each time; every host thread has its own."""
+
+    def __init__(self):
+        rows, rows8 = [Rows() for _ in range(3)], [Rows8() for _ in range(2)]
+        self.rows = [(d, ctypes.addressof(d)) for d in rows]
+        self.rows8 = [(d, ctypes.addressof(d)) for d in rows8]
+
+
+_descriptors = _Descriptors()
+_get_device = None
+
+
+def _current_device() -> int:
+    global _get_device
+    if _get_device is None:
+        import torch
+        if not torch.cuda.is_available():
+            return -1
+        torch.cuda.init()
+        _get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _get_device()
+
+
+def _matrix(t, name: str, device: int) -> Tuple[int, int, int]:
+    """(rows, columns, distance of rows) of a tensor read as rows of its last dimension."""
+    if t.get_device() != device or device < 0:
+        raise ValueError(f"{name} is on {t.device}, the current device is {'cuda:%d' % device if device >= 0 else 'no GPU'}")
+    shape, strides = t.shape, t.stride()
+    if len(shape) == 2:
+        rows, cols = shape
+        if strides[1] != 1 and cols > 1:
+            raise ValueError(f"{name}: the elements of a row must lie one behind the other")
+        return rows, cols, strides[0]
+    if len(shape) < 2 or not t.is_contiguous():
+        raise ValueError(f"{name}: expected two dimensions, or more in a contiguous tensor (an NHWC map)")
+    cols = shape[-1]
+    return (t.numel() // cols if cols else 0), cols, cols
+
+
+def _fill_rows(slot, t, name: str, device: int) -> int:
+    rows, cols, ld = _matrix(t, name, device)
+    _PACK_ROWS.pack_into(slot[0], 0, t.data_ptr(), rows, ld, cols, _dtype_code(t))
+    return slot[1]
+
+
+def _fill_rows8(slot, q, scale, name: str, device: int) -> int:
+    import torch
+    rows, cols, ld = _matrix(q, name, device)
+    if q.dtype is not torch.int8:
+        raise TypeError(f"{name} must be int8")
+    _vector(scale, name + "'s scales", rows, device)
+    _PACK_ROWS8.pack_into(slot[0], 0, q.data_ptr(), scale.data_ptr(), rows, ld, cols)
+    return slot[1]
+
+
+def _vector(t, name: str, n: int, device: int, types=None) -> int:
+    import torch
+    if t.dtype is not torch.float32 and (types is None or t.dtype not in types):
+        raise TypeError(f"{name}: unsupported dtype {t.dtype}")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: on {t.device}, the current device is cuda:{device}")
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name}: expected {n} values, one behind the other")
+    return t.data_ptr()
+
+
+def empty_rows8(rows: int, cols: int, device="cuda"):
+    """(q, scale) for `rows` rows of `cols` 8-bit values; rows start at multiples of 16 bytes, as the tensor cores need it."""
+    import torch
+    q = torch.empty((rows, (cols + 15) // 16 * 16), dtype=torch.int8, device=device)[:, :cols]
+    return q, torch.empty(rows, dtype=torch.float32, device=device)
+
+
+def quantize_rows(x, q, scale, stream=None) -> None:
+    """gdws_quantize_rows: rows of x (fp32 or bf16) to 8 bits in q (int8) with one fp32 scale each in `scale`."""
+    L, d, device = lib(), _descriptors, _current_device()
+    st = L.gdws_quantize_rows(_fill_rows(d.rows[0], x, "x", device), _fill_rows8(d.rows8[0], q, scale, "q", device), _stream(stream))
+    if st:
+        raise GdwsError(st, last_error())
+
+
+def norm_quantize_rows(x, q, scale, weight=None, eps: float = 1e-6, residual=None, total=None, stream=None) -> None:
+    """gdws_norm_quantize_rows: h = x + residual (written to `total`), 8 bits of h * weight / sqrt(mean h^2 + eps) in q and scale."""
+    L, d, device = lib(), _descriptors, _current_device()
+    px = _fill_rows(d.rows[0], x, "x", device)
+    pw = code = 0
+    if weight is not None:
+        code = _dtype_code(weight)
+        pw = _vector(weight, "weight", x.shape[-1], device, _dtypes)
+    st = L.gdws_norm_quantize_rows(px, None if residual is None else _fill_rows(d.rows[1], residual, "residual", device),
+                                   None if total is None else _fill_rows(d.rows[2], total, "total", device), pw or None, code, eps,
+                                   _fill_rows8(d.rows8[0], q, scale, "q", device), _stream(stream))
+    if st:
+        raise GdwsError(st, last_error())
+
+
+def dequantize_rows(q, scale, y, stream=None) -> None:
+    """gdws_dequantize_rows: y = q * scale (y: fp32 or bf16)."""
+    L, d, device = lib(), _descriptors, _current_device()
+    st = L.gdws_dequantize_rows(_fill_rows8(d.rows8[0], q, scale, "q", device), _fill_rows(d.rows[0], y, "y", device), _stream(stream))
+    if st:
+        raise GdwsError(st, last_error())
+
+
+def pointwise8(q, scale, w, w_scale, y, bias=None, relu: bool = False, stream=None) -> None:
+    """gdws_pointwise8: y = (q w^T) * w_scale * scale + bias for 8-bit rows q and 8-bit weights w [D][columns]; optionally ReLU."""
+    L, d, device = lib(), _descriptors, _current_device()
+    st = L.gdws_pointwise8(_fill_rows8(d.rows8[0], q, scale, "q", device), _fill_rows8(d.rows8[1], w, w_scale, "w", device),
+                           None if bias is None else _vector(bias, "bias", w.shape[0], device), int(relu),
+                           _fill_rows(d.rows[0], y, "y", device), _stream(stream))
+    if st:
+        raise GdwsError(st, last_error())
+
+
+def pointwise8_kernel(q, scale, w, w_scale, y) -> int:
+    """gdws_pointwise8_kernel: KERNEL8_* that this call takes."""
+    L, d, device, kernel = lib(), _descriptors, _current_device(), ctypes.c_int()
+    _check(L.gdws_pointwise8_kernel(_fill_rows8(d.rows8[0], q, scale, "q", device), _fill_rows8(d.rows8[1], w, w_scale, "w", device),
+                                    _fill_rows(d.rows[0], y, "y", device), ctypes.byref(kernel)))
+    return kernel.value
+
+
+def rows_status() -> None:
+    """gdws_rows_status: raises if a bounded wait of a call on rows ran out on the current device."""
+    _check(lib().gdws_rows_status())

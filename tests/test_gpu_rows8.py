@@ -1,0 +1,182 @@
+"""gdws_quantize_rows, gdws_norm_quantize_rows and gdws_dequantize_rows against their definitions in 64 bits: every q equal, sums
+of squares within the rounding of their fp32 additions, nothing written beside the rows."""
+import pytest
+import torch
+
+from paper_2110_14871_b200 import build as gbuild
+from paper_2110_14871_b200 import gdws
+
+from rows8_util import HALF, Field, steps_of
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    gbuild.build_library()
+
+
+def values(rows, cols, dtype, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn((rows, cols), generator=gen, device="cuda")
+    x *= torch.where(torch.rand(cols, generator=gen, device="cuda") < 0.02, 15.0, 1.0)
+    return x.to(TYPES[dtype])
+
+
+def field_of(x, ld=None, shift=0):
+    f = Field(x.shape[0], x.shape[1], x.dtype, ld, shift)
+    f.t.copy_(x)
+    return f
+
+
+# rows, cols; (extra elements between rows, first element's shift) of x and of q
+SHAPES = [(1, 1), (3, 7), (9, 64), (5, 256), (33, 257), (2, 512), (7, 513), (4, 1337), (3, 2048), (2, 2049), (1, 4096), (3, 4097), (2, 8192),
+          (2, 8193), (1, 16384), (2, 16391), (1, 32768), (2, 32769), (1, 70001)]
+GAPS = [((0, 0), (0, 0)), ((8, 0), (16, 0)), ((1, 0), (3, 1)), ((0, 1), (0, 0))]
+
+
+@pytest.mark.parametrize("gaps", range(len(GAPS)))
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_quantize(rows, cols, dtype, gaps):
+    (gx, sx), (gq, sq) = GAPS[gaps]
+    x = field_of(values(rows, cols, dtype, 7 * rows + cols), cols + gx, sx)
+    q, scale, y = Field(rows, cols, torch.int8, cols + gq, sq), Field(1, rows, torch.float32), Field(rows, cols, TYPES[dtype], cols + gx, sx)
+    gdws.quantize_rows(x.t, q.t, scale.t[0])
+    gdws.dequantize_rows(q.t, scale.t[0], y.t)
+    torch.cuda.synchronize()
+    want, want_scale = steps_of(x.t.float())
+    assert torch.equal(q.t, want) and torch.equal(scale.t[0], want_scale)
+    assert torch.equal(y.t, (want.float() * want_scale[:, None]).to(TYPES[dtype]))
+    for f, name in ((x, "x"), (q, "q"), (scale, "the scales"), (y, "y")):
+        f.check(name)
+
+
+def norm_bound(cols):
+    """Relative: a thread adds up at most max(32, cols / 1024 + 1) squares, ten additions join the threads' sums; the square root
+    halves what that amounts to.  Division by cols, eps, root, m / 127 and the quotient: five roundings."""
+    return ((max(32, cols // 1024 + 1) + 10) / 2 + 5.5) * 2.0 ** -24
+
+
+@pytest.mark.parametrize("residual,total,weight", [(True, "own", "f32"), (True, "residual", "bf16"), (False, None, "f32"), (True, "x", None), (False, "own", "bf16"), (True, None, "f32")])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols,gap,shift", [(1, 1, 0, 0), (5, 96, 0, 0), (9, 333, 0, 0), (300, 512, 8, 0), (3, 1536, 0, 0), (2, 2049, 7, 1), (2, 4096, 0, 0), (2, 8191, 0, 0), (1, 16384, 0, 0), (2, 33000, 0, 0),
+                                                 (1, 40001, 0, 1)])
+def test_norm_quantize(rows, cols, gap, shift, dtype, residual, total, weight):
+    eps = 1e-5
+    x = field_of(values(rows, cols, dtype, rows + cols), cols + gap, shift)
+    r = field_of(3 * values(rows, cols, dtype, rows + cols + 1), cols + gap, shift) if residual else None
+    w = (1 + 0.3 * values(1, cols, "f32", 5)[0]).to(TYPES[weight]) if weight else None
+    h = x.t.float() + r.t.float() if residual else x.t.float()
+    u = h * w.float() if weight else h
+    t = {None: None, "own": Field(rows, cols, TYPES[dtype], cols + gap, shift), "residual": r, "x": x}[total]
+    q, scale = Field(rows, cols, torch.int8, cols + gap, shift), Field(1, rows, torch.float32)
+    gdws.norm_quantize_rows(x.t, q.t, scale.t[0], weight=w, eps=eps, residual=r.t if residual else None, total=t.t if t else None)
+    torch.cuda.synchronize()
+    want, _ = steps_of(u)
+    assert torch.equal(q.t, want)
+    want_scale = u.double().abs().amax(1) / 127 / torch.sqrt(h.double().square().mean(1) + eps)
+    assert ((scale.t[0].double() - want_scale).abs() <= norm_bound(cols) * want_scale).all()
+    if t:
+        assert torch.equal(t.t, h.to(TYPES[dtype]))
+    for f in (x, r, t, q, scale):
+        if f:
+            f.check("a matrix")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_halfway_cases(dtype):
+    """Quotients that lie exactly between two integers, and next to it."""
+    u = torch.arange(-254, 255, device="cuda").float() / 2          # with 127 in the row: every second one is a tie
+    u = torch.stack([torch.cat([u, torch.tensor([127.0], device="cuda")]), torch.cat([u * 2 ** -9, torch.tensor([127.0 * 2 ** -9], device="cuda")])])
+    x = u.to(TYPES[dtype])
+    assert torch.equal(x.float(), u)
+    if dtype == "f32":      # one step of the type beside the ties
+        x = torch.cat([x, torch.nextafter(x, torch.full_like(x, 1e9)).clamp(-127, 127), torch.nextafter(x, torch.full_like(x, -1e9)).clamp(-127, 127)])
+    q, scale = gdws.empty_rows8(*x.shape)
+    gdws.quantize_rows(x, q, scale)
+    assert torch.equal(q, steps_of(x.float())[0])
+    x = values(64, 4096, dtype, 3)
+    x[:, ::5] = x.abs().amax(1, keepdim=True) / 2                     # 63.5 steps
+    q, scale = gdws.empty_rows8(*x.shape)
+    gdws.quantize_rows(x, q, scale)
+    assert torch.equal(q, steps_of(x.float())[0])
+
+
+@pytest.mark.parametrize("cols", [5, 256, 1000, 4096, 40000])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_zero_tiny_huge_and_not_finite(dtype, cols):
+    x = values(9, cols, dtype, 11)
+    x[0] = 0
+    x[1] *= 2.0 ** -120
+    x[2] = x[2].float().mul(2.0 ** -100).mul(2.0 ** -40).to(x.dtype)      # subnormal in either type
+    x[3] = (x[3].float() / x[3].float().abs().max()).to(x.dtype) * 2.0 ** 127
+    x[4, cols // 2] = float("inf")
+    x[5, cols - 1] = float("-inf")
+    x[6, 0] = float("nan")
+    x[7] = -0.0
+    w = torch.ones(cols, device="cuda")
+    for norm in (False, True):
+        q, scale = gdws.empty_rows8(9, cols)
+        if norm:
+            gdws.norm_quantize_rows(x, q, scale, weight=w)
+        else:
+            gdws.quantize_rows(x, q, scale)
+        want, want_scale = steps_of(x.float())
+        if norm:
+            want[3], want_scale[3] = 0, float("nan")                      # its squares pass fp32
+        assert torch.equal(q, want)
+        assert torch.equal(torch.isnan(scale), torch.isnan(want_scale)) and scale[0] == 0 and scale[7] == 0
+        if not norm:
+            assert torch.equal(scale.nan_to_num(-1), want_scale.nan_to_num(-1))
+        y = torch.empty((9, cols), device="cuda")
+        gdws.dequantize_rows(q, scale, y)
+        assert torch.isnan(y[4:7]).all() and not torch.isnan(y[:3]).any() and (y[0] == 0).all()
+
+
+def test_no_rows_and_views():
+    q, scale = gdws.empty_rows8(0, 40)
+    gdws.quantize_rows(torch.empty((0, 40), device="cuda"), q, scale)
+    gdws.norm_quantize_rows(torch.empty((0, 40), device="cuda"), q, scale)
+    gdws.dequantize_rows(q, scale, torch.empty((0, 40), device="cuda"))
+    # an NHWC map is rows of channels; x and total as columns of one buffer
+    x = values(2 * 5 * 3, 24, "bf16", 2)
+    qa, sa = torch.empty((2, 5, 3, 24), dtype=torch.int8, device="cuda"), torch.empty(30, device="cuda")
+    gdws.quantize_rows(x.view(2, 5, 3, 24), qa, sa)
+    assert torch.equal(qa.view(30, 24), steps_of(x.float())[0])
+    both = torch.zeros((30, 48), dtype=torch.bfloat16, device="cuda")
+    both[:, :24] = x
+    q, scale = gdws.empty_rows8(30, 24)
+    gdws.norm_quantize_rows(both[:, :24], q, scale, total=both[:, 24:])
+    assert torch.equal(both[:, 24:], x) and torch.equal(q, qa.view(30, 24))
+
+
+def test_streams_graphs_and_the_same_result_twice():
+    x, r = values(50, 1000, "bf16", 21), values(50, 1000, "bf16", 22)
+    q, scale = gdws.empty_rows8(50, 1000)
+    total, y = torch.empty_like(x), torch.empty_like(x)
+
+    def step():
+        gdws.norm_quantize_rows(x, q, scale, residual=r, total=total)
+        gdws.dequantize_rows(q, scale, y)
+
+    step()
+    want = [t.clone() for t in (q, scale, total, y)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        y.zero_()
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip((q, scale, total, y), want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for t in (q, scale, total, y):
+        t.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((q, scale, total, y), want))
+    assert HALF[torch.float32] == torch.finfo(torch.float32).eps / 2
