@@ -479,7 +479,7 @@ gdws_status_t gdws_quantize_rows(const gdws_rows_t *x, const gdws_rows8_t *q, vo
     st = rows_device(&device, &sms);
     if (st != GDWS_OK) return st;
     const cudaError_t e = launch_rows<false>(params_of(x, q), x->dtype == GDWS_F32, (cudaStream_t)stream);
-    return e == cudaSuccess ? GDWS_OK : cuda_fail(e, "rows8_kernel launch");
+    return launched(e, "rows8_kernel launch");
 }
 
 gdws_status_t gdws_norm_quantize_rows(const gdws_rows_t *x, const gdws_rows_t *residual, const gdws_rows_t *total, const void *weight,
@@ -518,7 +518,7 @@ gdws_status_t gdws_norm_quantize_rows(const gdws_rows_t *x, const gdws_rows_t *r
     if (residual) { P.residual = residual->ptr; P.ldr = residual->ld; }
     if (total) { P.total = total->ptr; P.ldt = total->ld; }
     const cudaError_t e = launch_rows<true>(P, x->dtype == GDWS_F32, (cudaStream_t)stream);
-    return e == cudaSuccess ? GDWS_OK : cuda_fail(e, "rows8_kernel launch");
+    return launched(e, "rows8_kernel launch");
 }
 
 gdws_status_t gdws_dequantize_rows(const gdws_rows8_t *q, const gdws_rows_t *y, void *stream)
@@ -535,7 +535,7 @@ gdws_status_t gdws_dequantize_rows(const gdws_rows8_t *q, const gdws_rows_t *y, 
     if (st != GDWS_OK) return st;
     ValuesParams P = {q->q, q->scale, y->ptr, q->ld, y->ld, (int)q->rows, q->cols};
     const cudaError_t e = y->dtype == GDWS_F32 ? launch_values<float>(P, (cudaStream_t)stream) : launch_values<__nv_bfloat16>(P, (cudaStream_t)stream);
-    return e == cudaSuccess ? GDWS_OK : cuda_fail(e, "values_kernel launch");
+    return launched(e, "values_kernel launch");
 }
 
 }  // extern "C"

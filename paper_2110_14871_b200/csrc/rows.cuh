@@ -12,4 +12,30 @@ gdws_status_t check_rows8(const char *call, const char *name, const gdws_rows8_t
 gdws_status_t check_pointwise8(const gdws_rows8_t *x, const gdws_rows8_t *w, const float *bias, const gdws_rows_t *y);
 gdws_status_t rows_device(int *device, int *sms);       // the current device, checked to be compute capability 10.x, and its SMs
 
+// A launch's result as a status; a refused launch leaves no error behind for the caller's next CUDA call.
+inline gdws_status_t launched(cudaError_t e, const char *what)
+{
+    if (e == cudaSuccess) return GDWS_OK;
+    cudaGetLastError();
+    return cuda_fail(e, what);
+}
+
+// A wait on arrivals from both blocks of a pair: acquire at cluster scope, bounded like the others.
+static __device__ __noinline__ void mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *status, int code)
+{
+    for (uint32_t it = 0; it < kSpinLimit; ++it) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        if (ok) return;
+        if (it > 4096) __nanosleep(64);
+        if ((it & 1023) == 0 && *abort_flag) return;
+    }
+    *abort_flag = 1;
+    atomicOr(status, code);
+}
+
 }  // namespace gdws
