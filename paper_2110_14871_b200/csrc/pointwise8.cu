@@ -1,4 +1,6 @@
 // The pointwise product on rows in 8 bits: y[r,d] = (sum_c x[r,c] w[d,c]) * ws[d] * xs[r] + bias[d].
+#include <math.h>
+
 #include <atomic>
 
 #include "rows.cuh"
@@ -8,24 +10,23 @@ namespace {
 
 __device__ int g_rows_status;        // status word of the calls on rows, one per device
 
-// fp32 in the order that the interface names; NaN stays NaN.
-__device__ __forceinline__ float finish8(int sum, float ws, float xs, float bias, int relu)
+// fp32 in the order that the interface names.  floor: 0 with ReLU, else -infinity; NaN stays NaN.
+__device__ __forceinline__ float finish8(int sum, float ws, float xs, float bias, float floor)
 {
-    const float v = fmaf((float)sum * ws, xs, bias);
-    return relu && v < 0.f ? 0.f : v;
+    float v = fmaf((float)sum * ws, xs, bias);
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(floor));
+    return v;
 }
-__device__ __forceinline__ void store8(void *y, bool f32, int64_t at, float v)
-{
-    if (f32) ((float *)y)[at] = v;
-    else ((__nv_bfloat16 *)y)[at] = __float2bfloat16_rn(v);
-}
+__device__ __forceinline__ void store8(float *y, float v) { *y = v; }
+__device__ __forceinline__ void store8(__nv_bfloat16 *y, float v) { *y = __float2bfloat16_rn(v); }
 
 struct P8Params {
     const int8_t *x, *w;
     const float *xs, *ws, *bias;
     void *y;
     int64_t ldx, ldw, ldy;
-    int rows, K, D, relu;
+    float floor;
+    int rows, K, D;
     bool out_f32;
 };
 
@@ -43,6 +44,7 @@ __device__ __forceinline__ int load4(const int8_t *row, int k, int K, bool words
     return v;
 }
 
+template <typename Y>
 __global__ void __launch_bounds__(256) p8_alu_kernel(const __grid_constant__ P8Params P, int tiles_d)
 {
     grid_launch_dependents();
@@ -80,7 +82,7 @@ __global__ void __launch_bounds__(256) p8_alu_kernel(const __grid_constant__ P8P
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int r = r0 + ty + 16 * i;
-            if (r < P.rows) store8(P.y, P.out_f32, (int64_t)r * P.ldy + d, finish8(acc[i][j], ws, P.xs[r], bias, P.relu));
+            if (r < P.rows) store8((Y *)P.y + (int64_t)r * P.ldy + d, finish8(acc[i][j], ws, P.xs[r], bias, P.floor));
         }
     }
 }
@@ -89,7 +91,7 @@ gdws_status_t p8_alu(const P8Params &P, cudaStream_t st)
 {
     const int64_t tiles_d = ((int64_t)P.D + 63) / 64, tiles = ((int64_t)P.rows + 63) / 64 * tiles_d;
     if (tiles > 0x7fffffff) return fail(GDWS_ERR_UNSUPPORTED, "gdws_pointwise8: %d x %d outputs are more than one launch covers", P.rows, P.D);
-    const cudaError_t e = launch_overlapped(p8_alu_kernel, dim3((unsigned)tiles), 256u, 0, st, P, (int)tiles_d);
+    const cudaError_t e = launch_overlapped(P.out_f32 ? p8_alu_kernel<float> : p8_alu_kernel<__nv_bfloat16>, dim3((unsigned)tiles), 256u, 0, st, P, (int)tiles_d);
     return launched(e, "p8_alu_kernel launch");
 }
 
@@ -111,7 +113,8 @@ struct alignas(64) P8TcParams {
     const float *xs, *ws, *bias;
     void *y;
     int64_t ldy;
-    int rows, D, relu, out_f32;
+    float floor;
+    int rows, D;
     int pieces;                      // of 128 columns
     int nt, tiles_r, split, ns, stage_bytes;      // slices
     int tiles_d, nitems, band;                    // pairs
@@ -151,6 +154,7 @@ __device__ __forceinline__ void st_cluster(uint32_t addr, int v)
 // Few outputs: a cluster of `split` blocks shares a tile of 128 channels x nt rows, each block sums a slice of the columns.  The
 // partial sums are integers, so that adding them up in any order gives the same bits: each block sends its sums of column c of
 // the tile to block c / (nt / split), which adds them and stores.
+template <typename Y>
 __global__ void __launch_bounds__(256, 1) p8_slices_kernel(const __grid_constant__ P8TcParams P)
 {
     extern __shared__ uint8_t smem_raw[];
@@ -228,16 +232,16 @@ __global__ void __launch_bounds__(256, 1) p8_slices_kernel(const __grid_constant
     tc_fence_after();
 
     const uint32_t t_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-    auto put = [&](int c, int sum) {      // column c of the tile, channel d
-        if (r0 + c < P.rows && d < P.D) store8(P.y, P.out_f32, (int64_t)(r0 + c) * P.ldy + d, finish8(sum, ws, xs_s[c], bias, P.relu));
-    };
+    Y *const y = (Y *)P.y + (int64_t)r0 * P.ldy + d;
+    const int live = d < P.D ? P.rows - r0 : 0;      // columns of the tile that this lane stores
     if (P.split == 1) {
         for (int c = (warp >> 2) * 8; c < P.nt; c += 16) {
             uint32_t acc[8];
             tmem_ld8(t_base + (uint32_t)c, acc);
             tmem_ld_wait();
 #pragma unroll
-            for (int e = 0; e < 8; ++e) put(c + e, (int)acc[e]);
+            for (int e = 0; e < 8; ++e)
+                if (c + e < live) store8(y + (c + e) * P.ldy, finish8((int)acc[e], ws, xs_s[c + e], bias, P.floor));
         }
     } else {
         const int per = P.nt / P.split;             // columns that a block stores
@@ -257,7 +261,8 @@ __global__ void __launch_bounds__(256, 1) p8_slices_kernel(const __grid_constant
         for (int c = tid >> 7; c < per; c += 2) {
             int sum = 0;
             for (int o = 0; o < P.split; ++o) sum += recv[(o * per + c) * 128 + (tid & 127)];
-            put(rank * per + c, sum);
+            const int at = rank * per + c;
+            if (at < live) store8(y + at * P.ldy, finish8(sum, ws, xs_s[at], bias, P.floor));
         }
     }
     tc_fence_before();
@@ -282,6 +287,7 @@ __device__ __forceinline__ P8Tile pair_tile(const P8TcParams &P, int item)
     return {d * 256, (b * P.band + in - d * h) * 256};
 }
 
+template <typename Y>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) p8_pairs_kernel(const __grid_constant__ P8TcParams P)
 {
     extern __shared__ uint8_t smem_raw[];
@@ -386,11 +392,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) p8_
                 tmem_ld32(t_base + (uint32_t)c, acc);
                 tmem_ld_wait();
                 const float *xs = &xs_s[buf][half * 128 + c];
-                const int64_t at = (int64_t)(t.r0 + half * 128 + c) * P.ldy + d;
+                Y *y = (Y *)P.y + (int64_t)(t.r0 + half * 128 + c) * P.ldy + d;
                 if (d < P.D) {
+                    // no condition between the columns of a whole block: 32 independent chains
+                    if (c + 32 <= live) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if (c + e < live) store8(P.y, P.out_f32, at + e * P.ldy, finish8((int)acc[e], ws, xs[e], bias, P.relu));
+                        for (int e = 0; e < 32; ++e, y += P.ldy) store8(y, finish8((int)acc[e], ws, xs[e], bias, P.floor));
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e, y += P.ldy)
+                            if (c + e < live) store8(y, finish8((int)acc[e], ws, xs[e], bias, P.floor));
+                    }
                 }
             }
             tc_fence_before();
@@ -459,12 +471,15 @@ gdws_status_t p8_tc(const P8Params &A, const P8Choice &c, int device, int sms, c
     gdws_status_t rc = rows_map(&P.tw, A.w, A.D, A.K, ldw, 128, device);
     if (rc == GDWS_OK) rc = rows_map(&P.tx, A.x, A.rows, A.K, ldx, pairs ? 128 : c.nt, device);
     if (rc != GDWS_OK) return rc;
-    P.xs = A.xs; P.ws = A.ws; P.bias = A.bias; P.y = A.y; P.ldy = A.ldy; P.rows = A.rows; P.D = A.D; P.relu = A.relu; P.out_f32 = A.out_f32;
+    P.xs = A.xs; P.ws = A.ws; P.bias = A.bias; P.y = A.y; P.ldy = A.ldy; P.rows = A.rows; P.D = A.D; P.floor = A.floor;
     P.pieces = (A.K + kPiece - 1) / kPiece;
     static std::atomic<bool> allowed[64];
     if (!allowed[device].load(std::memory_order_acquire)) {      // once per device: the full dynamic shared memory
-        cudaError_t e = cudaFuncSetAttribute(p8_slices_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(p8_pairs_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmem);
+        const cudaFuncAttribute most = cudaFuncAttributeMaxDynamicSharedMemorySize;
+        cudaError_t e = cudaFuncSetAttribute(p8_slices_kernel<float>, most, kMaxSmem);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(p8_slices_kernel<__nv_bfloat16>, most, kMaxSmem);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(p8_pairs_kernel<float>, most, kPairSmem);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(p8_pairs_kernel<__nv_bfloat16>, most, kPairSmem);
         if (e != cudaSuccess) return launched(e, "cudaFuncSetAttribute(pointwise8)");
         allowed[device].store(true, std::memory_order_release);
     }
@@ -475,7 +490,7 @@ gdws_status_t p8_tc(const P8Params &A, const P8Choice &c, int device, int sms, c
         if (items > 0x3fffffff) return fail(GDWS_ERR_UNSUPPORTED, "gdws_pointwise8: %d x %d outputs are more than one launch covers", A.rows, A.D);
         P.nitems = (int)items; P.band = 8;
         const unsigned grid = 2u * (unsigned)std::min<int64_t>(items, sms / 2);
-        e = launch_overlapped(p8_pairs_kernel, dim3(grid), (unsigned)kPairThreads, kPairSmem, st, P);
+        e = launch_overlapped(A.out_f32 ? p8_pairs_kernel<float> : p8_pairs_kernel<__nv_bfloat16>, dim3(grid), (unsigned)kPairThreads, kPairSmem, st, P);
     } else {
         P.nt = c.nt; P.split = c.split; P.tiles_r = (int)(((int64_t)A.rows + c.nt - 1) / c.nt);
         const int64_t blocks = ((int64_t)A.D + 127) / 128 * P.tiles_r * c.split;
@@ -495,7 +510,7 @@ gdws_status_t p8_tc(const P8Params &A, const P8Choice &c, int device, int sms, c
         attr[1].id = cudaLaunchAttributeClusterDimension;
         attr[1].val.clusterDim.x = (unsigned)c.split; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
         cfg.attrs = attr; cfg.numAttrs = c.split > 1 ? 2 : 1;
-        e = cudaLaunchKernelEx(&cfg, p8_slices_kernel, P);
+        e = A.out_f32 ? cudaLaunchKernelEx(&cfg, p8_slices_kernel<float>, P) : cudaLaunchKernelEx(&cfg, p8_slices_kernel<__nv_bfloat16>, P);
     }
     return launched(e, pairs ? "p8_pairs_kernel launch" : "p8_slices_kernel launch");
 }
@@ -506,7 +521,7 @@ P8Params p8_params(const gdws_rows8_t *x, const gdws_rows8_t *w, const float *bi
     P8Params P;
     P.x = x->q; P.w = w->q; P.xs = x->scale; P.ws = w->scale; P.bias = bias; P.y = y->ptr;
     P.ldx = x->rows > 1 ? x->ld : x->cols; P.ldw = w->rows > 1 ? w->ld : w->cols; P.ldy = y->rows > 1 ? y->ld : y->cols;
-    P.rows = (int)x->rows; P.K = x->cols; P.D = (int)w->rows; P.relu = relu != 0; P.out_f32 = y->dtype == GDWS_F32;
+    P.rows = (int)x->rows; P.K = x->cols; P.D = (int)w->rows; P.floor = relu ? 0.f : -INFINITY; P.out_f32 = y->dtype == GDWS_F32;
     return P;
 }
 
