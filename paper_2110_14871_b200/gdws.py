@@ -64,9 +64,6 @@ class Rows8(ctypes.Structure):
     _fields_ = [("q", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("rows", ctypes.c_int64), ("ld", ctypes.c_int64), ("cols", ctypes.c_int)]
 
 
-_PACK_ROWS, _PACK_ROWS8 = struct.Struct("@Pqqii"), struct.Struct("@PPqqi4x")
-assert _PACK_ROWS.size == ctypes.sizeof(Rows) and _PACK_ROWS8.size == ctypes.sizeof(Rows8)
-
 _lib = None
 
 
@@ -376,68 +373,91 @@ class Plan:
 
 # ---- rows in 8 bits
 
+# The descriptors of a call lie one behind the other and are packed at once: three of gdws_rows_t, then two of gdws_rows8_t (of
+# which a call may use fewer).  A small call's time is that of these lines, so they ask a tensor for nothing twice.
+_ROWS, _ROWS8 = "Pqqii", "PPqqi4x"
+_QUANTIZE, _NORM, _PRODUCT = (struct.Struct("@" + f).pack_into for f in (_ROWS + _ROWS8, 3 * _ROWS + _ROWS8, _ROWS + 2 * _ROWS8))
+_ROWS_SIZE, _ROWS8_SIZE = ctypes.sizeof(Rows), ctypes.sizeof(Rows8)
+assert struct.calcsize("@" + _ROWS) == _ROWS_SIZE and struct.calcsize("@" + _ROWS8) == _ROWS8_SIZE
+
+
 class _Descriptors(threading.local):
-    """Descriptors of one call, filled anew each time; every host thread has its own."""
+    """Memory for the descriptors of one call, filled anew each time; every host thread has its own."""
 
     def __init__(self):
-        rows, rows8 = [Rows() for _ in range(3)], [Rows8() for _ in range(2)]
-        self.rows = [(d, ctypes.addressof(d)) for d in rows]
-        self.rows8 = [(d, ctypes.addressof(d)) for d in rows8]
+        self.buffer = ctypes.create_string_buffer(3 * _ROWS_SIZE + 2 * _ROWS8_SIZE)
+        at = ctypes.addressof(self.buffer)
+        r, r2 = at + _ROWS_SIZE, at + 2 * _ROWS_SIZE
+        self.quantize = (at, r)                                          # x or y, q
+        self.norm = (at, r, r2, r2 + _ROWS_SIZE)                         # x, residual, total, q
+        self.product = (at, r, r + _ROWS8_SIZE)                          # y, x, w
 
 
 _descriptors = _Descriptors()
-_get_device = None
+_rows_lib = None       # the library, once torch has initialised CUDA
+_get_device = _get_stream = None
+_int8 = _float32 = None
 
 
-def _current_device() -> int:
-    global _get_device
-    if _get_device is None:
-        import torch
-        if not torch.cuda.is_available():
-            return -1
-        torch.cuda.init()
-        _get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-    return _get_device()
+def _rows_setup():
+    """The library; on a host without a GPU the calls then refuse every tensor."""
+    global _rows_lib, _get_device, _get_stream, _int8, _float32
+    import torch
+    L = lib()
+    _dtype_code(torch.empty(0, dtype=torch.float32))
+    _int8, _float32 = torch.int8, torch.float32
+    if not torch.cuda.is_available():
+        _get_device = lambda: -1  # noqa: E731
+        return L
+    torch.cuda.init()
+    _get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    _get_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+    _rows_lib = L
+    return L
 
 
-def _matrix(t, name: str, device: int) -> Tuple[int, int, int]:
-    """(rows, columns, distance of rows) of a tensor read as rows of its last dimension."""
+def _not_on(t, name: str, device: int):
+    return ValueError(f"{name} is on {t.device}, the current device is {'cuda:%d' % device if device >= 0 else 'no GPU'}")
+
+
+def _geometry(t, name: str, device: int):
+    """(address, rows, distance of rows, columns) of a tensor read as rows of its last dimension."""
     if t.get_device() != device or device < 0:
-        raise ValueError(f"{name} is on {t.device}, the current device is {'cuda:%d' % device if device >= 0 else 'no GPU'}")
-    shape, strides = t.shape, t.stride()
+        raise _not_on(t, name, device)
+    shape = t.shape
     if len(shape) == 2:
         rows, cols = shape
-        if strides[1] != 1 and cols > 1:
+        ld, one = t.stride()
+        if one != 1 and cols > 1:
             raise ValueError(f"{name}: the elements of a row must lie one behind the other")
-        return rows, cols, strides[0]
+        return t.data_ptr(), rows, ld, cols
     if len(shape) < 2 or not t.is_contiguous():
         raise ValueError(f"{name}: expected two dimensions, or more in a contiguous tensor (an NHWC map)")
     cols = shape[-1]
-    return (t.numel() // cols if cols else 0), cols, cols
+    return t.data_ptr(), (t.numel() // cols if cols else 0), cols, cols
 
 
-def _fill_rows(slot, t, name: str, device: int) -> int:
-    rows, cols, ld = _matrix(t, name, device)
-    _PACK_ROWS.pack_into(slot[0], 0, t.data_ptr(), rows, ld, cols, _dtype_code(t))
-    return slot[1]
-
-
-def _fill_rows8(slot, q, scale, name: str, device: int) -> int:
-    import torch
-    rows, cols, ld = _matrix(q, name, device)
-    if q.dtype is not torch.int8:
-        raise TypeError(f"{name} must be int8")
-    _vector(scale, name + "'s scales", rows, device)
-    _PACK_ROWS8.pack_into(slot[0], 0, q.data_ptr(), scale.data_ptr(), rows, ld, cols)
-    return slot[1]
-
-
-def _vector(t, name: str, n: int, device: int, types=None) -> int:
-    import torch
-    if t.dtype is not torch.float32 and (types is None or t.dtype not in types):
+def _values(t, name: str, device: int):
+    """The fields of gdws_rows_t."""
+    code = _dtypes.get(t.dtype)
+    if code is None:
         raise TypeError(f"{name}: unsupported dtype {t.dtype}")
+    return *_geometry(t, name, device), code
+
+
+def _steps(q, scale, name: str, device: int):
+    """The fields of gdws_rows8_t."""
+    if q.dtype is not _int8:
+        raise TypeError(f"{name} must be int8")
+    at, rows, ld, cols = _geometry(q, name, device)
+    return at, _vector(scale, name + "'s scales", rows, device), rows, ld, cols
+
+
+def _vector(t, name: str, n: int, device: int) -> int:
+    if t.dtype is not _float32:
+        raise TypeError(f"{name}: expected float32, got {t.dtype}")
     if t.get_device() != device:
-        raise ValueError(f"{name}: on {t.device}, the current device is cuda:{device}")
+        raise _not_on(t, name, device)
     if t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name}: expected {n} values, one behind the other")
     return t.data_ptr()
@@ -452,50 +472,71 @@ def empty_rows8(rows: int, cols: int, device="cuda"):
 
 def quantize_rows(x, q, scale, stream=None) -> None:
     """gdws_quantize_rows: rows of x (fp32 or bf16) to 8 bits in q (int8) with one fp32 scale each in `scale`."""
-    L, d, device = lib(), _descriptors, _current_device()
-    st = L.gdws_quantize_rows(_fill_rows(d.rows[0], x, "x", device), _fill_rows8(d.rows8[0], q, scale, "q", device), _stream(stream))
+    L = _rows_lib or _rows_setup()
+    device, d = _get_device(), _descriptors
+    _QUANTIZE(d.buffer, 0, *_values(x, "x", device), *_steps(q, scale, "q", device))
+    px, pq = d.quantize
+    st = L.gdws_quantize_rows(px, pq, _get_stream(device) if stream is None else _stream(stream))
     if st:
         raise GdwsError(st, last_error())
 
 
+_NO_ROWS = (0, 0, 0, 0, 0)
+
+
 def norm_quantize_rows(x, q, scale, weight=None, eps: float = 1e-6, residual=None, total=None, stream=None) -> None:
     """gdws_norm_quantize_rows: h = x + residual (written to `total`), 8 bits of h * weight / sqrt(mean h^2 + eps) in q and scale."""
-    L, d, device = lib(), _descriptors, _current_device()
-    px = _fill_rows(d.rows[0], x, "x", device)
-    pw = code = 0
+    L = _rows_lib or _rows_setup()
+    device, d = _get_device(), _descriptors
+    _NORM(d.buffer, 0, *_values(x, "x", device), *(_NO_ROWS if residual is None else _values(residual, "residual", device)),
+          *(_NO_ROWS if total is None else _values(total, "total", device)), *_steps(q, scale, "q", device))
+    w = code = None
     if weight is not None:
-        code = _dtype_code(weight)
-        pw = _vector(weight, "weight", x.shape[-1], device, _dtypes)
-    st = L.gdws_norm_quantize_rows(px, None if residual is None else _fill_rows(d.rows[1], residual, "residual", device),
-                                   None if total is None else _fill_rows(d.rows[2], total, "total", device), pw or None, code, eps,
-                                   _fill_rows8(d.rows8[0], q, scale, "q", device), _stream(stream))
+        code = _dtypes.get(weight.dtype)
+        if code is None:
+            raise TypeError(f"weight: unsupported dtype {weight.dtype}")
+        if weight.get_device() != device:
+            raise _not_on(weight, "weight", device)
+        if weight.numel() != x.shape[-1] or not weight.is_contiguous():
+            raise ValueError(f"weight: expected {x.shape[-1]} values, one behind the other")
+        w = weight.data_ptr()
+    px, pr, pt, pq = d.norm
+    st = L.gdws_norm_quantize_rows(px, None if residual is None else pr, None if total is None else pt, w, code or 0, eps, pq,
+                                   _get_stream(device) if stream is None else _stream(stream))
     if st:
         raise GdwsError(st, last_error())
 
 
 def dequantize_rows(q, scale, y, stream=None) -> None:
     """gdws_dequantize_rows: y = q * scale (y: fp32 or bf16)."""
-    L, d, device = lib(), _descriptors, _current_device()
-    st = L.gdws_dequantize_rows(_fill_rows8(d.rows8[0], q, scale, "q", device), _fill_rows(d.rows[0], y, "y", device), _stream(stream))
+    L = _rows_lib or _rows_setup()
+    device, d = _get_device(), _descriptors
+    _QUANTIZE(d.buffer, 0, *_values(y, "y", device), *_steps(q, scale, "q", device))
+    py, pq = d.quantize
+    st = L.gdws_dequantize_rows(pq, py, _get_stream(device) if stream is None else _stream(stream))
     if st:
         raise GdwsError(st, last_error())
 
 
 def pointwise8(q, scale, w, w_scale, y, bias=None, relu: bool = False, stream=None) -> None:
     """gdws_pointwise8: y = (q w^T) * w_scale * scale + bias for 8-bit rows q and 8-bit weights w [D][columns]; optionally ReLU."""
-    L, d, device = lib(), _descriptors, _current_device()
-    st = L.gdws_pointwise8(_fill_rows8(d.rows8[0], q, scale, "q", device), _fill_rows8(d.rows8[1], w, w_scale, "w", device),
-                           None if bias is None else _vector(bias, "bias", w.shape[0], device), int(relu),
-                           _fill_rows(d.rows[0], y, "y", device), _stream(stream))
+    L = _rows_lib or _rows_setup()
+    device, d = _get_device(), _descriptors
+    _PRODUCT(d.buffer, 0, *_values(y, "y", device), *_steps(q, scale, "q", device), *_steps(w, w_scale, "w", device))
+    py, px, pw = d.product
+    st = L.gdws_pointwise8(px, pw, None if bias is None else _vector(bias, "bias", y.shape[-1], device), relu, py,
+                           _get_stream(device) if stream is None else _stream(stream))
     if st:
         raise GdwsError(st, last_error())
 
 
 def pointwise8_kernel(q, scale, w, w_scale, y) -> int:
     """gdws_pointwise8_kernel: KERNEL8_* that this call takes."""
-    L, d, device, kernel = lib(), _descriptors, _current_device(), ctypes.c_int()
-    _check(L.gdws_pointwise8_kernel(_fill_rows8(d.rows8[0], q, scale, "q", device), _fill_rows8(d.rows8[1], w, w_scale, "w", device),
-                                    _fill_rows(d.rows[0], y, "y", device), ctypes.byref(kernel)))
+    L = _rows_lib or _rows_setup()
+    device, d, kernel = _get_device(), _descriptors, ctypes.c_int()
+    _PRODUCT(d.buffer, 0, *_values(y, "y", device), *_steps(q, scale, "q", device), *_steps(w, w_scale, "w", device))
+    py, px, pw = d.product
+    _check(L.gdws_pointwise8_kernel(px, pw, py, ctypes.byref(kernel)))
     return kernel.value
 
 
