@@ -385,7 +385,8 @@ typedef enum {
     GDWS_KERNEL8_NONE = 0,   /* no rows: nothing is launched                                          */
     GDWS_KERNEL8_ALU = 1,    /* any alignment                                                         */
     GDWS_KERNEL8_SLICES = 2, /* tensor cores, few outputs: clusters share a tile's sum                */
-    GDWS_KERNEL8_PAIRS = 3   /* tensor cores, many outputs: pairs of SMs share 256 x 256 of them      */
+    GDWS_KERNEL8_PAIRS = 3,  /* tensor cores, many outputs: pairs of SMs share 256 x 256 of them      */
+    GDWS_KERNEL8_FEW = 4     /* at most 8 rows: w read once, four-byte dot products                   */
 } gdws_kernel8_t;
 /* gdws_pointwise8_kernel -- the kernel that this call takes on the current device (a B200 where there is none).  Diagnostic, host only. */
 GDWS_API gdws_status_t gdws_pointwise8_kernel(const gdws_rows8_t *x, const gdws_rows8_t *w, const gdws_rows_t *y, int *kernel);

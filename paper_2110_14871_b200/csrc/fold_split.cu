@@ -274,8 +274,7 @@ void cluster_capacities(int device, int sms, int (&most)[kMostSlices + 1])
 
 int cluster_capacity(const gdws_plan_s *p, int split)
 {
-    static constexpr int b200[kMostSlices + 1] = {0, kB200Sms, 74, 45, 33, 26, 22, 15, 15};      // as a B200 answers: for queries on a host without a GPU
-    return p->device >= 0 ? p->clusters[split] : b200[split];
+    return p->device >= 0 ? p->clusters[split] : kB200Clusters[split];
 }
 
 namespace {

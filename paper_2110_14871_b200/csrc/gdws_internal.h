@@ -239,6 +239,7 @@ inline int gdw_stage_of(const gdws_plan_s *p)
 
 // SMs of the plan's device; a plan built without a device (host-side queries only) assumes a B200's 148.
 constexpr int kB200Sms = 148;
+constexpr int kB200Clusters[kMostSlices + 1] = {0, kB200Sms, 74, 45, 33, 26, 22, 15, 15};      // as a B200 answers cluster_capacities
 inline int sm_count_of(const gdws_plan_s *p) { return p->sm_count > 0 ? p->sm_count : kB200Sms; }
 
 // f32.cu

@@ -3,6 +3,7 @@
 #include <math.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "rows.cuh"
 
@@ -120,7 +121,7 @@ struct RowsParams {
     int64_t ldx, ldr, ldt, ldq;
     float eps;
     int rows, cols;
-    bool weight_f32;
+    bool weight_f32, weight_whole;      // weight_whole: on a boundary of 16 bytes
 };
 
 __device__ __forceinline__ float to_float(float v) { return v; }
@@ -128,89 +129,136 @@ __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162f
 __device__ __forceinline__ void from_float(float v, float &o) { o = v; }
 __device__ __forceinline__ void from_float(float v, __nv_bfloat16 &o) { o = __float2bfloat16_rn(v); }
 
-// VEC consecutive values (VEC > 1: as 16-byte pieces where all of them exist; zeros from `cols` on).
+// Two fp32 operations in one instruction; each rounds as the single one.
+__device__ __forceinline__ void mul2(float &a, float &b, float x, float y)
+{
+    asm("{\n\t.reg .b64 p, q;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %3};\n\tmul.rn.f32x2 p, p, q;\n\tmov.b64 {%0, %1}, p;\n\t}" : "+f"(a), "+f"(b) : "f"(x), "f"(y));
+}
+__device__ __forceinline__ void add2(float &a, float &b, float x, float y)
+{
+    asm("{\n\t.reg .b64 p, q;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %3};\n\tadd.rn.f32x2 p, p, q;\n\tmov.b64 {%0, %1}, p;\n\t}" : "+f"(a), "+f"(b) : "f"(x), "f"(y));
+}
+__device__ __forceinline__ void square2(float &a, float &b, float x, float y)      // a += x^2, b += y^2
+{
+    asm("{\n\t.reg .b64 p, q;\n\tmov.b64 p, {%0, %1};\n\tmov.b64 q, {%2, %3};\n\tfma.rn.f32x2 p, q, q, p;\n\tmov.b64 {%0, %1}, p;\n\t}" : "+f"(a), "+f"(b) : "f"(x), "f"(y));
+}
+// The larger of a and |b|; a NaN stays.
+__device__ __forceinline__ float larger(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(fabsf(b)));
+    return r;
+}
+
+// VEC consecutive values as they lie in memory (VEC > 1: 16-byte pieces where all of them exist; zeros from `cols` on).
 template <int VEC, typename T>
-__device__ __forceinline__ void load_vec(const T *row, int c, int cols, float (&v)[VEC])
+union Raw {
+    uint4 w[VEC == 1 ? 1 : VEC * sizeof(T) / 16];
+    T e[VEC];
+    __device__ __forceinline__ Raw() {}
+};
+// whole: all of them exist and lie on a boundary of 16 bytes.  Others are taken one by one; c may be negative.
+template <int VEC, typename T>
+__device__ __forceinline__ void load_raw(const T *row, int c, int cols, bool whole, Raw<VEC, T> &b)
 {
     if constexpr (VEC == 1) {
-        v[0] = c < cols ? to_float(row[c]) : 0.f;
+        from_float(0.f, b.e[0]);
+        if (c < cols) b.e[0] = row[c];
     } else {
-        if (c + VEC <= cols) {
-            union { uint4 w[VEC * sizeof(T) / 16]; T e[VEC]; } b;
+        constexpr int kPieces = (int)(VEC * sizeof(T) / 16);
 #pragma unroll
-            for (int i = 0; i < (int)(VEC * sizeof(T) / 16); ++i) b.w[i] = reinterpret_cast<const uint4 *>(row + c)[i];
+        for (int i = 0; i < kPieces; ++i) b.w[i] = make_uint4(0, 0, 0, 0);
+        if (whole) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) v[e] = to_float(b.e[e]);
+            for (int i = 0; i < kPieces; ++i) b.w[i] = reinterpret_cast<const uint4 *>(row + c)[i];
         } else {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) v[e] = c + e < cols ? to_float(row[c + e]) : 0.f;
+            for (int e = 0; e < VEC; ++e)
+                if ((unsigned)(c + e) < (unsigned)cols) b.e[e] = row[c + e];
         }
     }
 }
 template <int VEC, typename T>
-__device__ __forceinline__ void store_vec(T *row, int c, int cols, const float (&v)[VEC])
+__device__ __forceinline__ void store_vec(T *row, int c, int cols, bool whole, const float (&v)[VEC])
 {
     if constexpr (VEC == 1) {
         if (c < cols) from_float(v[0], row[c]);
     } else {
-        if (c + VEC <= cols) {
-            union { uint4 w[VEC * sizeof(T) / 16]; T e[VEC]; } b;
+        Raw<VEC, T> b;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) from_float(v[e], b.e[e]);
+        for (int e = 0; e < VEC; ++e) from_float(v[e], b.e[e]);
+        if (whole) {
 #pragma unroll
             for (int i = 0; i < (int)(VEC * sizeof(T) / 16); ++i) reinterpret_cast<uint4 *>(row + c)[i] = b.w[i];
         } else {
 #pragma unroll
             for (int e = 0; e < VEC; ++e)
-                if (c + e < cols) from_float(v[e], row[c + e]);
+                if ((unsigned)(c + e) < (unsigned)cols) row[c + e] = b.e[e];
         }
     }
 }
 
-// What a row's elements are divided by.  m: max |u| (finite).  Magnitudes below 2^-60 are lifted by 2^64, which is exact, so that
-// 127 / m stays in range.
-struct Steps {
-    float lift, m, inv;
-    __device__ __forceinline__ explicit Steps(float most)
-    {
-        lift = most < 0x1p-60f ? 0x1p64f : 1.f;
-        m = most * lift;
-        inv = m > 0.f ? 127.f / m : 0.f;
-    }
-};
-// 127 u / m rounded to the nearest integer.  u * inv is off by at most 127 * 2^-23 = 1.5e-5 from the quotient: where it lies that
-// close to the middle of two integers (one element of 16000 at random), the exact comparison of 254 |u| with (2 j + 1) m decides;
-// both are products of a 24-bit and an 8-bit number, exact in fp64.  kMagic brings the integer into the low mantissa bits.
+// 127 u / m rounded to the nearest integer, m = max |u|.  t = u * inv (inv = 127 / m, rounded) is off by at most 127 * 2^-23 = 1.5e-5
+// from the quotient; kMagic brings its integer r into the low mantissa bits.  Where t lies that close to the middle between r and
+// its neighbour (one fp32 number of 16000 at random; bf16 numbers often lie on it), the sign of 254 u - (2 r +- 1) m decides.  It is
+// exact: 254 u is taken in two terms, and what is left of the difference has a few bits.  (All times 2^-8, so that nothing overflows.)
 constexpr float kMagic = 12582912.f, kNear = 0.5f - 3e-5f;
-template <int VEC>
-__device__ __forceinline__ void quantize_vec(const float (&u)[VEC], const Steps &s, int (&q)[VEC])
+// m as the divisions take it, and what u is multiplied with before: magnitudes below 2^-60 are lifted by 2^64, which is exact, so
+// that 127 / m stays in range.
+__device__ __forceinline__ float lifted(float &m)
 {
-    float t[VEC], far = 0.f;
+    const float lift = m < 0x1p-60f ? 0x1p64f : 1.f;
+    m *= lift;
+    return lift;
+}
+// q, the integer that t was rounded to, or its neighbour; d = t minus that integer.
+__device__ __forceinline__ int exact_step(float u, float m, float t, float d, int q)
+{
+    const float s = copysignf(1.f, d), k = fmaf(2.f, t - d, s) * 0x1p-8f;
+    const float a = u * (254.f / 256.f), a2 = fmaf(u, 254.f / 256.f, -a);
+    const float past = (fmaf(-k, m, a) + a2) * s;          // how far the quotient lies beyond the middle
+    return past > 0.f || (past == 0.f && (q & 1)) ? q + (int)s : q;
+}
+template <int N>
+__device__ __forceinline__ void quantize(const float (&u)[N], float m, float inv, int (&q)[N])
+{
+    float t[N], far = 0.f;
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-        t[e] = u[e] * s.lift * s.inv;
-        const float r = t[e] + kMagic;
-        q[e] = __float_as_int(r);
-        far = fmaxf(far, fabsf(t[e] - (r - kMagic)));
+    for (int e = 0; e < N; ++e) t[e] = u[e];
+    if constexpr (N % 2 == 0) {
+#pragma unroll
+        for (int e = 0; e < N; e += 2) {
+            mul2(t[e], t[e + 1], inv, inv);
+            float r0 = t[e], r1 = t[e + 1], d0 = t[e], d1 = t[e + 1];
+            add2(r0, r1, kMagic, kMagic);
+            q[e] = __float_as_int(r0);
+            q[e + 1] = __float_as_int(r1);
+            add2(r0, r1, -kMagic, -kMagic);
+            add2(d0, d1, -r0, -r1);
+            far = fmaxf(fmaxf(far, fabsf(d0)), fabsf(d1));
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            t[e] *= inv;
+            const float r = t[e] + kMagic;
+            q[e] = __float_as_int(r);
+            far = fmaxf(far, fabsf(t[e] - (r - kMagic)));
+        }
     }
     if (far > kNear) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            const float r = t[e] + kMagic;
-            if (fabsf(t[e] - (r - kMagic)) > kNear) {
-                const int j = (int)fabsf(t[e]);
-                const double a = 254.0 * (double)fabsf(u[e] * s.lift), b = (double)(2 * j + 1) * (double)s.m;
-                const int n = a > b || (a == b && (j & 1)) ? j + 1 : j;
-                q[e] = t[e] < 0.f ? -n : n;
-            }
+        for (int e = 0; e < N; ++e) {
+            const float d = t[e] - ((t[e] + kMagic) - kMagic);
+            if (fabsf(d) > kNear) q[e] = exact_step(u[e], m, t[e], d, q[e]);
         }
     }
 }
 template <int VEC>
-__device__ __forceinline__ void store_steps(int8_t *row, int c, int cols, const int (&q)[VEC])
+__device__ __forceinline__ void store_steps(int8_t *row, int c, int cols, bool whole, const int *q)
 {
     if constexpr (VEC == 8) {
-        if (c + 8 <= cols) {
+        if (whole) {
             uint2 w;
             w.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
             w.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
@@ -220,17 +268,47 @@ __device__ __forceinline__ void store_steps(int8_t *row, int c, int cols, const 
     }
 #pragma unroll
     for (int e = 0; e < VEC; ++e)
-        if (c + e < cols) row[c + e] = (int8_t)q[e];
+        if ((unsigned)(c + e) < (unsigned)cols) row[c + e] = (int8_t)q[e];
 }
 
-// Largest magnitude (as bits: infinity and NaN compare above every finite value) and sum of squares over the TPR threads of a row.
+// The same where q's vectors lie `by` bytes before its boundaries of 8 bytes: a lane stores the word that begins inside its
+// vector, with the first bytes of the next lane's; what no such word covers goes byte by byte.  All lanes of a warp take part.
+template <int TPR>
+__device__ __forceinline__ void store_steps_across(int8_t *row, int c, int cols, int by, bool live, bool whole, const int (&q)[8])
+{
+    uint32_t lo = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+    uint32_t hi = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
+    const uint64_t mine = (uint64_t)hi << 32 | lo;
+    const uint64_t next = (uint64_t)__shfl_down_sync(0xffffffffu, hi, 1) << 32 | __shfl_down_sync(0xffffffffu, lo, 1);
+    if (!live) return;
+    if (!by) return store_steps<8>(row, c, cols, whole, q);
+    constexpr int kLanes = TPR < 32 ? TPR : 32;
+    const int lane = threadIdx.x & (kLanes - 1);
+    const bool word = lane != kLanes - 1 && c + by >= 0 && c + by + 8 <= cols;
+    const bool before = lane != 0 && c - 8 + by >= 0 && c + by <= cols;         // the lane before stores this one's first bytes
+    if (word) *reinterpret_cast<uint64_t *>(row + c + by) = mine >> (8 * by) | next << (64 - 8 * by);
+    if (!word || !before) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if ((e < by ? !before : !word) && (unsigned)(c + e) < (unsigned)cols) row[c + e] = (int8_t)q[e];
+    }
+}
+
+// Largest magnitude (as bits: infinity and NaN compare above every finite value) and sum of squares over the TPR threads of a row;
+// all threads of a warp take part.
 template <int TPR, bool NORM>
 __device__ __forceinline__ void reduce_row(uint32_t &most, float &squares)
 {
-    most = __reduce_max_sync(0xffffffffu, most);
+    constexpr int kLanes = TPR < 32 ? TPR : 32;
+    if constexpr (kLanes == 32) {
+        most = __reduce_max_sync(0xffffffffu, most);
+    } else {
+#pragma unroll
+        for (int o = kLanes / 2; o; o >>= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+    }
     if (NORM) {
 #pragma unroll
-        for (int o = 16; o; o >>= 1) squares += __shfl_xor_sync(0xffffffffu, squares, o);
+        for (int o = kLanes / 2; o; o >>= 1) squares += __shfl_xor_sync(0xffffffffu, squares, o);
     }
     if constexpr (TPR > 32) {
         constexpr int kWarps = TPR / 32;
@@ -248,83 +326,155 @@ __device__ __forceinline__ void reduce_row(uint32_t &most, float &squares)
     }
 }
 
-// A row's scale from its largest |u| and its sum of squares; false: the row is not finite.
 template <bool NORM>
-__device__ __forceinline__ bool row_scale(uint32_t most, float squares, const RowsParams &P, float *scale)
+__device__ __forceinline__ bool finite_row(uint32_t most, float squares) { return most < 0x7f800000u && (!NORM || squares < INFINITY); }
+template <bool NORM>
+__device__ __forceinline__ float row_scale(uint32_t most, float squares, const RowsParams &P)
 {
-    const bool fine = most < 0x7f800000u && (!NORM || squares < INFINITY);
-    *scale = __uint_as_float(most) / 127.f;
-    if (NORM) *scale /= sqrtf(squares / (float)P.cols + P.eps);
-    if (!fine) *scale = __uint_as_float(0x7fffffffu);
-    return fine;
+    float scale = __uint_as_float(most) / 127.f;
+    if (NORM) scale /= sqrtf(squares / (float)P.cols + P.eps);
+    return finite_row<NORM>(most, squares) ? scale : __uint_as_float(0x7fffffffu);
 }
 
-template <bool NORM, int VEC, typename T>
-__device__ __forceinline__ void load_sum(const RowsParams &P, int64_t r, int c, float (&h)[VEC], float (&u)[VEC])
-{
-    load_vec<VEC>((const T *)P.x + r * P.ldx, c, P.cols, h);
-    if (NORM && P.residual) {
-        float a[VEC];
-        load_vec<VEC>((const T *)P.residual + r * P.ldr, c, P.cols, a);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) h[e] += a[e];
+// VEC values of a row: x, what is added to it and what multiplies it, and from them h and u.
+template <typename T, int VEC, bool NORM>
+struct Piece {
+    Raw<VEC, T> x, residual;
+    float weight[VEC];
+    __device__ __forceinline__ void load(const RowsParams &P, int64_t r, int c, bool whole)
+    {
+        load_raw<VEC>((const T *)P.x + r * P.ldx, c, P.cols, whole, x);
+        if (NORM && P.residual) load_raw<VEC>((const T *)P.residual + r * P.ldr, c, P.cols, whole, residual);
     }
+    // shift: how far before a multiple of VEC the row's vectors begin, the same for all threads of a row
+    __device__ __forceinline__ void load_weight(const RowsParams &P, int c, bool whole, int shift)
+    {
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) u[e] = h[e];
-    if (NORM && P.weight) {
-        float a[VEC];
-        if (P.weight_f32) load_vec<VEC>((const float *)P.weight, c, P.cols, a);
-        else load_vec<VEC>((const __nv_bfloat16 *)P.weight, c, P.cols, a);
+        for (int e = 0; e < VEC; ++e) weight[e] = 1.f;
+        if (!NORM || !P.weight) return;
+        if constexpr (VEC == 8) {
+            // fp32 weights at an odd place: three aligned pieces, moved down by one and by two
+            const int off = c & 3;
+            if (shift && P.weight_f32 && P.weight_whole && c >= off && c - off + 12 <= P.cols) {
+                float w[12];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) u[e] *= a[e];
+                for (int i = 0; i < 3; ++i) {
+                    const float4 v = reinterpret_cast<const float4 *>((const float *)P.weight + c - off)[i];
+                    w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
+                }
+#pragma unroll
+                for (int e = 0; e < 11; ++e) w[e] = off & 1 ? w[e + 1] : w[e];
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) weight[e] = off & 2 ? w[e + 2] : w[e];
+                return;
+            }
+        }
+        whole = whole && shift == 0 && P.weight_whole;
+        if (P.weight_f32) {
+            Raw<VEC, float> w;
+            load_raw<VEC>((const float *)P.weight, c, P.cols, whole, w);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) weight[e] = w.e[e];
+        } else {
+            Raw<VEC, __nv_bfloat16> w;
+            load_raw<VEC>((const __nv_bfloat16 *)P.weight, c, P.cols, whole, w);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) weight[e] = to_float(w.e[e]);
+        }
     }
-}
+    // h and u of these values, h stored as total, the row's largest |u| and sum of squares
+    __device__ __forceinline__ void values(const RowsParams &P, int64_t r, int c, bool whole, bool store, float *u, float &most, float (&squares)[2]) const
+    {
+        float h[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) h[e] = to_float(x.e[e]);
+        if (NORM && P.residual) {
+            if constexpr (VEC == 1) h[0] += to_float(residual.e[0]);
+            else
+#pragma unroll
+                for (int e = 0; e < VEC; e += 2) add2(h[e], h[e + 1], to_float(residual.e[e]), to_float(residual.e[e + 1]));
+        }
+        if (NORM && store) store_vec<VEC>((T *)P.total + r * P.ldt, c, P.cols, whole, h);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) u[e] = h[e];
+        if (NORM) {
+            if constexpr (VEC == 1) {
+                u[0] *= weight[0];
+                squares[0] = fmaf(h[0], h[0], squares[0]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < VEC; e += 2) {
+                    mul2(u[e], u[e + 1], weight[e], weight[e + 1]);
+                    square2(squares[0], squares[1], h[e], h[e + 1]);
+                }
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) most = larger(most, u[e]);
+    }
+};
 
-// One pass: TPR threads hold a row in registers, N values each, in vectors of VEC.
-template <typename T, int VEC, int N, int TPR, bool NORM>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) rows8_kernel(const __grid_constant__ RowsParams P)
+// One pass: TPR threads hold a row in registers, N values each, in vectors of VEC.  Everything is asked for before the first store:
+// total may be x's or the residual's memory for all that the compiler knows.  SHIFTED: rows start anywhere (contiguous rows of an odd
+// length); the vectors are those of the memory, a row's first begins up to VEC - 1 values before it, and x, residual and total
+// have to lie alike.  The weight's values and, where q's rows lie otherwise, the 8-bit ones are then taken one by one.
+template <typename T, int VEC, bool SHIFTED, int N, int TPR, bool NORM>
+__global__ void __launch_bounds__(TPR < 64 ? 128 : TPR) rows8_kernel(const __grid_constant__ RowsParams P)
 {
+    constexpr int kPer = TPR < 64 ? 128 / TPR : 1, kPieces = N / VEC;
     grid_launch_dependents();
     grid_dependency_wait();
-    const int64_t r = TPR < 256 ? (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR : blockIdx.x;
-    if (r >= P.rows) return;
+    int64_t r = (int64_t)blockIdx.x * kPer + threadIdx.x / TPR;
+    const bool live = r < P.rows;                    // a group behind the last row goes through that one again and stores nothing
+    if (!live) r = P.rows - 1;
     const int t = threadIdx.x % TPR;
-    float u[N / VEC][VEC];
-    uint32_t most = 0;
-    float squares = 0.f;
+    int8_t *const qrow = P.q + r * P.ldq;
+    const int shift = SHIFTED ? (int)((uintptr_t)((const T *)P.x + r * P.ldx) % 16 / sizeof(T)) : 0;
+    const int by = SHIFTED ? (int)((8 - ((uintptr_t)qrow - (uintptr_t)shift) % 8) % 8) : 0;      // from q's vectors to its next boundary of 8 bytes
+    auto column = [&](int i) { return (t + i * TPR) * VEC - shift; };
+    auto whole = [&](int c) { return VEC > 1 && (!SHIFTED || c >= 0) && c + VEC <= P.cols; };
+    float u[N], most = 0.f, squares[2] = {};
+    {
+        Piece<T, VEC, NORM> p[kPieces];
 #pragma unroll
-    for (int i = 0; i < N / VEC; ++i) {
-        const int c = (t + i * TPR) * VEC;
-        float h[VEC];
-        if (c < P.cols) {
-            load_sum<NORM, VEC, T>(P, r, c, h, u[i]);
-            if (NORM && P.total) store_vec<VEC>((T *)P.total + r * P.ldt, c, P.cols, h);
-        } else {
+        for (int i = 0; i < kPieces; ++i) p[i].load(P, r, column(i), whole(column(i)));
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) h[e] = u[i][e] = 0.f;
-        }
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            most = max(most, __float_as_uint(u[i][e]) & 0x7fffffffu);
-            if (NORM) squares = fmaf(h[e], h[e], squares);
+        for (int i = 0; i < kPieces; ++i) {
+            const int c = column(i);
+            p[i].load_weight(P, c, whole(c), shift);
+            p[i].values(P, r, c, whole(c), live && P.total, u + i * VEC, most, squares);
         }
     }
-    reduce_row<TPR, NORM>(most, squares);
-    float scale;
-    const bool fine = row_scale<NORM>(most, squares, P, &scale);
-    if (t == 0) P.scale[r] = scale;
-    const Steps s(fine ? __uint_as_float(most) : 0.f);
+    uint32_t top = __float_as_uint(most);
+    squares[0] += squares[1];
+    reduce_row<TPR, NORM>(top, squares[0]);
+    if (t == 0 && live) P.scale[r] = row_scale<NORM>(top, squares[0], P);
+    const bool fine = finite_row<NORM>(top, squares[0]);
+    float m = fine ? __uint_as_float(top) : 0.f;
+    const float lift = lifted(m), inv = m > 0.f ? 127.f / m : 0.f;
+    if (lift != 1.f || !fine) {
 #pragma unroll
-    for (int i = 0; i < N / VEC; ++i) {
-        const int c = (t + i * TPR) * VEC;
-        if (c >= P.cols) break;
-        int q[VEC];
-        if (!fine) {
+        for (int e = 0; e < N; ++e) u[e] = fine ? u[e] * lift : 0.f;
+    }
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) u[i][e] = 0.f;
+    for (int g = 0; g < N; g += 8) {
+        float v[8];
+        int q[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = u[g + e];
+        quantize<8>(v, m, inv, q);
+        if constexpr (SHIFTED) {
+            if (__any_sync(0xffffffffu, by != 0)) {          // a warp's rows may lie differently
+                const int c = column(g / VEC);
+                store_steps_across<TPR>(qrow, c, P.cols, by, live, whole(c), q);
+                continue;
+            }
         }
-        quantize_vec<VEC>(u[i], s, q);
-        store_steps<VEC>(P.q + r * P.ldq, c, P.cols, q);
+#pragma unroll
+        for (int e = 0; e < 8; e += VEC) {
+            const int c = column((g + e) / VEC);
+            if (live) store_steps<VEC>(qrow, c, P.cols, whole(c), q + e);
+        }
     }
 }
 
@@ -336,58 +486,95 @@ __global__ void __launch_bounds__(1024) rows8_long_kernel(const __grid_constant_
     grid_launch_dependents();
     grid_dependency_wait();
     const int64_t r = blockIdx.x;
-    uint32_t most = 0;
-    float squares = 0.f;
+    float most = 0.f, squares[2] = {};
     for (int c = threadIdx.x; c < P.cols; c += 1024) {
-        float h[1], u[1];
-        load_sum<NORM, 1, T>(P, r, c, h, u);
-        most = max(most, __float_as_uint(u[0]) & 0x7fffffffu);
-        if (NORM) squares = fmaf(h[0], h[0], squares);
+        Piece<T, 1, NORM> p;
+        float u[1];
+        p.load(P, r, c, false);
+        p.load_weight(P, c, false, 0);
+        p.values(P, r, c, false, false, u, most, squares);
     }
-    reduce_row<1024, NORM>(most, squares);
-    float scale;
-    const bool fine = row_scale<NORM>(most, squares, P, &scale);
-    if (threadIdx.x == 0) P.scale[r] = scale;
-    const Steps s(fine ? __uint_as_float(most) : 0.f);
+    uint32_t top = __float_as_uint(most);
+    reduce_row<1024, NORM>(top, squares[0]);
+    if (threadIdx.x == 0) P.scale[r] = row_scale<NORM>(top, squares[0], P);
+    const bool fine = finite_row<NORM>(top, squares[0]);
+    float m = fine ? __uint_as_float(top) : 0.f;
+    const float lift = lifted(m), inv = m > 0.f ? 127.f / m : 0.f;
     for (int c = threadIdx.x; c < P.cols; c += 1024) {
-        float h[1], u[1];
+        Piece<T, 1, NORM> p;
+        float u[1];
         int q[1];
-        load_sum<NORM, 1, T>(P, r, c, h, u);
-        if (NORM && P.total) store_vec<1>((T *)P.total + r * P.ldt, c, P.cols, h);
-        if (!fine) u[0] = 0.f;
-        quantize_vec<1>(u, s, q);
-        store_steps<1>(P.q + r * P.ldq, c, P.cols, q);
+        p.load(P, r, c, false);
+        p.load_weight(P, c, false, 0);
+        p.values(P, r, c, false, P.total != nullptr, u, most, squares);
+        u[0] = fine ? u[0] * lift : 0.f;
+        quantize<1>(u, m, inv, q);
+        store_steps<1>(P.q + r * P.ldq, c, P.cols, false, q);
     }
 }
 
-template <typename T, int VEC, int N, int TPR, bool NORM>
+template <typename T, int VEC, bool SHIFTED, int N, int TPR, bool NORM>
 cudaError_t launch_rows(const RowsParams &P, cudaStream_t st)
 {
-    constexpr int per = TPR < 256 ? 256 / TPR : 1;
-    return launch_overlapped(rows8_kernel<T, VEC, N, TPR, NORM>, dim3((unsigned)((P.rows + per - 1) / per)), TPR < 256 ? 256u : (unsigned)TPR, 0, st, P);
+    constexpr int per = TPR < 64 ? 128 / TPR : 1;
+    return launch_overlapped(rows8_kernel<T, VEC, SHIFTED, N, TPR, NORM>, dim3((unsigned)(((int64_t)P.rows + per - 1) / per)), TPR < 64 ? 128u : (unsigned)TPR, 0, st, P);
 }
-template <typename T, int VEC, bool NORM>
-cudaError_t launch_rows(const RowsParams &P, cudaStream_t st)
+// Values and threads for a row.  With many rows few threads with many values each: loads in flight, and what a row costs every
+// thread (sums, divisions) spread over them (8192 x 4096 bf16, norm: 128 threads 45.3 us, 256 47.3, 512 78).  With few rows, where
+// the chip is not full anyway, more threads.
+template <typename T, bool SHIFTED, bool NORM>
+cudaError_t launch_rows(const RowsParams &P, bool few, cudaStream_t st)
 {
-    if (P.cols <= 256) return launch_rows<T, VEC, 8, 32, NORM>(P, st);
-    if (P.cols <= 512) return launch_rows<T, VEC, 16, 32, NORM>(P, st);
-    if (P.cols <= 2048) return launch_rows<T, VEC, 8, 256, NORM>(P, st);
-    if (P.cols <= 4096) return launch_rows<T, VEC, 16, 256, NORM>(P, st);
-    if (P.cols <= 8192) return launch_rows<T, VEC, 8, 1024, NORM>(P, st);
-    if (P.cols <= 16384) return launch_rows<T, VEC, 16, 1024, NORM>(P, st);
-    if (P.cols <= 32768) return launch_rows<T, VEC, 32, 1024, NORM>(P, st);
+    const int n = P.cols + (SHIFTED ? 7 : 0);
+    if (few && n > 256) {
+        if (n <= 1024) return launch_rows<T, 8, SHIFTED, 8, 128, NORM>(P, st);
+        if (n <= 4096) return launch_rows<T, 8, SHIFTED, 8, 512, NORM>(P, st);
+    }
+    if (n <= 32) return launch_rows<T, 8, SHIFTED, 16, 2, NORM>(P, st);
+    if (n <= 64) return launch_rows<T, 8, SHIFTED, 16, 4, NORM>(P, st);
+    if (n <= 128) return launch_rows<T, 8, SHIFTED, 16, 8, NORM>(P, st);
+    if (n <= 256) return launch_rows<T, 8, SHIFTED, 16, 16, NORM>(P, st);
+    if (n <= 512) return launch_rows<T, 8, SHIFTED, 16, 32, NORM>(P, st);
+    if (n <= 768) return launch_rows<T, 8, SHIFTED, 24, 32, NORM>(P, st);
+    if (n <= 1024) return launch_rows<T, 8, SHIFTED, 32, 32, NORM>(P, st);
+    if (n <= 1536) return launch_rows<T, 8, SHIFTED, 24, 64, NORM>(P, st);
+    if (n <= 2048) return launch_rows<T, 8, SHIFTED, 32, 64, NORM>(P, st);
+    if (n <= 4096) return launch_rows<T, 8, SHIFTED, 32, 128, NORM>(P, st);
+    if (n <= 6144) return launch_rows<T, 8, SHIFTED, 24, 256, NORM>(P, st);
+    if (n <= 8192) return launch_rows<T, 8, SHIFTED, 32, 256, NORM>(P, st);
+    if (n <= 12288) return launch_rows<T, 8, SHIFTED, 24, 512, NORM>(P, st);
+    if (n <= 16384) return launch_rows<T, 8, SHIFTED, 32, 512, NORM>(P, st);
+    if (n <= 32768) return launch_rows<T, 8, SHIFTED, 32, 1024, NORM>(P, st);
     return launch_overlapped(rows8_long_kernel<T, NORM>, dim3((unsigned)P.rows), 1024u, 0, st, P);
 }
-template <bool NORM>
-cudaError_t launch_rows(const RowsParams &P, bool f32, cudaStream_t st)
+// Rows that lie neither on boundaries of 16 bytes nor alike, and shifted ones of which the vectors cut off at either end are a large
+// part (300000 x 30 bf16: 60 us by vectors): one value at a time.
+template <typename T, bool NORM>
+cudaError_t launch_single(const RowsParams &P, cudaStream_t st)
 {
-    // 16-byte pieces of the inputs and 8-byte ones of q where every row starts on such a boundary
-    const int64_t unit = f32 ? 4 : 8;
-    auto whole = [&](const void *p, int64_t ld) { return !((uintptr_t)p & 15) && (P.rows == 1 || ld % unit == 0); };
-    const bool vec = whole(P.x, P.ldx) && (!P.residual || whole(P.residual, P.ldr)) && (!P.total || whole(P.total, P.ldt)) && !((uintptr_t)P.weight & 15) &&
-                     !((uintptr_t)P.q & 7) && (P.rows == 1 || P.ldq % 8 == 0);
-    if (f32) return vec ? launch_rows<float, 8, NORM>(P, st) : launch_rows<float, 1, NORM>(P, st);
-    return vec ? launch_rows<__nv_bfloat16, 8, NORM>(P, st) : launch_rows<__nv_bfloat16, 1, NORM>(P, st);
+    if (P.cols <= 32) return launch_rows<T, 1, false, 8, 4, NORM>(P, st);
+    if (P.cols <= 64) return launch_rows<T, 1, false, 8, 8, NORM>(P, st);
+    if (P.cols <= 256) return launch_rows<T, 1, false, 8, 32, NORM>(P, st);
+    if (P.cols <= 1024) return launch_rows<T, 1, false, 8, 128, NORM>(P, st);
+    if (P.cols <= 4096) return launch_rows<T, 1, false, 8, 512, NORM>(P, st);
+    if (P.cols <= 16384) return launch_rows<T, 1, false, 16, 1024, NORM>(P, st);
+    return launch_overlapped(rows8_long_kernel<T, NORM>, dim3((unsigned)P.rows), 1024u, 0, st, P);
+}
+template <typename T, bool NORM>
+cudaError_t launch_typed(const RowsParams &P, int sms, cudaStream_t st)
+{
+    const int64_t unit = 16 / sizeof(T);
+    auto whole = [&](const void *p, int64_t ld) { return !p || (!((uintptr_t)p & 15) && (P.rows == 1 || ld % unit == 0)); };
+    auto alike = [&](const void *p, int64_t ld) { return !p || ((uintptr_t)p % 16 == (uintptr_t)P.x % 16 && (P.rows == 1 || (ld - P.ldx) % unit == 0)); };
+    const bool few = P.rows <= 2 * sms;
+    if (whole(P.x, P.ldx) && whole(P.residual, P.ldr) && whole(P.total, P.ldt) && !((uintptr_t)P.q & 7) && (P.rows == 1 || P.ldq % 8 == 0))
+        return launch_rows<T, false, NORM>(P, few, st);
+    return P.cols > 64 && alike(P.residual, P.ldr) && alike(P.total, P.ldt) ? launch_rows<T, true, NORM>(P, few, st) : launch_single<T, NORM>(P, st);
+}
+template <bool NORM>
+cudaError_t launch_rows(const RowsParams &P, bool f32, int sms, cudaStream_t st)
+{
+    return f32 ? launch_typed<float, NORM>(P, sms, st) : launch_typed<__nv_bfloat16, NORM>(P, sms, st);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -397,51 +584,85 @@ struct ValuesParams {
     const int8_t *q;
     const float *scale;
     void *y;
-    int64_t ldq, ldy;
-    int rows, cols;
+    int64_t ldq, ldy, pieces;        // pieces of VEC values in all
+    int cols, per_row;               // pieces of a row
+    uint32_t dv_row[2];              // divisions by per_row
 };
 
-// blockDim: x along a row, y rows.
-template <typename T, int VEC>
+// VEC 8-bit values (8 or 4) in a word.
+template <int VEC>
+struct Steps {
+    typedef typename std::conditional<VEC == 8, uint64_t, uint32_t>::type word;
+};
+// Columns c to c + VEC - 1 of a row, zeros for those that it does not have.  ALIGNED: they lie on a boundary of VEC bytes.
+template <int VEC, bool ALIGNED>
+__device__ __forceinline__ typename Steps<VEC>::word load_steps(const int8_t *row, int c, int cols)
+{
+    typedef typename Steps<VEC>::word Word;
+    const int off = ALIGNED ? 0 : (int)((uintptr_t)(row + c) % VEC);
+    if ((ALIGNED || c >= 0) && c + VEC <= cols && off == 0) return *reinterpret_cast<const Word *>(row + c);
+    if (!ALIGNED && off && c >= off && c - off + 2 * VEC <= cols) {           // two aligned words of the row
+        const Word *a = reinterpret_cast<const Word *>(row + c - off);
+        return a[0] >> (8 * off) | a[1] << (8 * (VEC - off));
+    }
+    Word w = 0;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e)
+        if ((unsigned)(c + e) < (unsigned)cols) w |= (Word)(uint8_t)row[c + e] << (8 * e);
+    return w;
+}
+
+// A block takes 256 * kAhead pieces in a row, whatever rows they belong to, and asks for all of them before it stores.  A piece is
+// what a 16-byte store of y takes; SHIFTED: rows of y start anywhere, a row's first piece before it (as in rows8_kernel).
+template <typename T, bool SHIFTED>
 __global__ void __launch_bounds__(256) values_kernel(const __grid_constant__ ValuesParams P)
 {
+    constexpr int VEC = 16 / sizeof(T), kAhead = 4;
     grid_launch_dependents();
     grid_dependency_wait();
-    const int64_t r = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
-    if (r >= P.rows) return;
-    const float s = P.scale[r];
-    const int8_t *q = P.q + r * P.ldq;
-    T *y = (T *)P.y + r * P.ldy;
-    for (int c = threadIdx.x * VEC; c < P.cols; c += blockDim.x * VEC) {
+    const int64_t first = (int64_t)blockIdx.x * (256 * kAhead), row0 = first / P.per_row;
+    const int in_row = (int)(first - row0 * P.per_row), here = (int)min(P.pieces - first, (int64_t)(256 * kAhead));
+    typename Steps<VEC>::word q[kAhead];
+    float s[kAhead];
+    // the i-th piece of this thread: its row, and its first column; false: there is none
+    auto piece = [&](int i, int64_t &row, int &c) {
+        const int at = i * 256 + (int)threadIdx.x, dr = div_by(in_row + at, P.dv_row);
+        row = row0 + dr;
+        c = (in_row + at - dr * P.per_row) * VEC;
+        if (SHIFTED) c -= (int)((uintptr_t)((T *)P.y + row * P.ldy) % 16 / sizeof(T));
+        return at < here;
+    };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+        int64_t row;
+        int c;
+        if (!piece(i, row, c)) break;
+        s[i] = P.scale[row];
+        q[i] = load_steps<VEC, !SHIFTED>(P.q + row * P.ldq, c, P.cols);
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+        int64_t row;
+        int c;
+        if (!piece(i, row, c)) break;
         float v[VEC];
-        if (VEC == 8 && c + 8 <= P.cols) {
-            union { uint2 w; int8_t e[8]; } b;
-            b.w = *reinterpret_cast<const uint2 *>(q + c);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) v[e] = (float)b.e[e] * s;
-        } else {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) v[e] = c + e < P.cols ? (float)q[c + e] * s : 0.f;
-        }
-        store_vec<VEC>(y, c, P.cols, v);
+        for (int e = 0; e < VEC; ++e) v[e] = (float)(int8_t)(q[i] >> (8 * e)) * s[i];
+        store_vec<VEC>((T *)P.y + row * P.ldy, c, P.cols, (!SHIFTED || c >= 0) && c + VEC <= P.cols, v);
     }
 }
 
 template <typename T>
-cudaError_t launch_values(const ValuesParams &P, cudaStream_t st)
+cudaError_t launch_values(ValuesParams P, int64_t rows, cudaStream_t st)
 {
-    const bool vec = !((uintptr_t)P.q & 7) && !((uintptr_t)P.y & 15) && (P.rows == 1 || (P.ldq % 8 == 0 && P.ldy % (16 / (int64_t)sizeof(T)) == 0));
-    const int64_t n = vec ? (P.cols + 7) / 8 : P.cols;
-    unsigned tx = 1;
-    while (tx < 256 && tx < n) tx *= 2;
-    const unsigned ty = 256 / tx;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(((unsigned)P.rows + ty - 1) / ty); cfg.blockDim = dim3(tx, ty); cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr; cfg.numAttrs = 1;
-    return vec ? cudaLaunchKernelEx(&cfg, values_kernel<T, 8>, P) : cudaLaunchKernelEx(&cfg, values_kernel<T, 1>, P);
+    constexpr int kVec = 16 / sizeof(T);
+    const bool whole = !((uintptr_t)P.q % kVec) && !((uintptr_t)P.y & 15) && (rows == 1 || (P.ldq % kVec == 0 && P.ldy % kVec == 0));
+    P.per_row = (int)(((int64_t)P.cols + kVec - 1 + (whole ? 0 : kVec - 1)) / kVec);
+    P.pieces = rows * P.per_row;
+    div_magic(P.per_row, P.dv_row);
+    const int64_t blocks = (P.pieces + 1023) / 1024;
+    if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    return launch_overlapped(whole ? values_kernel<T, false> : values_kernel<T, true>, dim3((unsigned)blocks), 256u, 0, st, P);
 }
 
 gdws_status_t same_shape(const char *call, const char *name, int64_t rows, int cols, const gdws_rows8_t *q)
@@ -478,7 +699,7 @@ gdws_status_t gdws_quantize_rows(const gdws_rows_t *x, const gdws_rows8_t *q, vo
     int device, sms;
     st = rows_device(&device, &sms);
     if (st != GDWS_OK) return st;
-    const cudaError_t e = launch_rows<false>(params_of(x, q), x->dtype == GDWS_F32, (cudaStream_t)stream);
+    const cudaError_t e = launch_rows<false>(params_of(x, q), x->dtype == GDWS_F32, sms, (cudaStream_t)stream);
     return launched(e, "rows8_kernel launch");
 }
 
@@ -514,10 +735,10 @@ gdws_status_t gdws_norm_quantize_rows(const gdws_rows_t *x, const gdws_rows_t *r
     st = rows_device(&device, &sms);
     if (st != GDWS_OK) return st;
     RowsParams P = params_of(x, q);
-    P.eps = eps; P.weight = weight; P.weight_f32 = weight_dtype == GDWS_F32;
+    P.eps = eps; P.weight = weight; P.weight_f32 = weight_dtype == GDWS_F32; P.weight_whole = !((uintptr_t)weight & 15);
     if (residual) { P.residual = residual->ptr; P.ldr = residual->ld; }
     if (total) { P.total = total->ptr; P.ldt = total->ld; }
-    const cudaError_t e = launch_rows<true>(P, x->dtype == GDWS_F32, (cudaStream_t)stream);
+    const cudaError_t e = launch_rows<true>(P, x->dtype == GDWS_F32, sms, (cudaStream_t)stream);
     return launched(e, "rows8_kernel launch");
 }
 
@@ -533,8 +754,9 @@ gdws_status_t gdws_dequantize_rows(const gdws_rows8_t *q, const gdws_rows_t *y, 
     int device, sms;
     st = rows_device(&device, &sms);
     if (st != GDWS_OK) return st;
-    ValuesParams P = {q->q, q->scale, y->ptr, q->ld, y->ld, (int)q->rows, q->cols};
-    const cudaError_t e = y->dtype == GDWS_F32 ? launch_values<float>(P, (cudaStream_t)stream) : launch_values<__nv_bfloat16>(P, (cudaStream_t)stream);
+    ValuesParams P = {};
+    P.q = q->q; P.scale = q->scale; P.y = y->ptr; P.ldq = q->ld; P.ldy = y->ld; P.cols = q->cols;
+    const cudaError_t e = y->dtype == GDWS_F32 ? launch_values<float>(P, q->rows, (cudaStream_t)stream) : launch_values<__nv_bfloat16>(P, q->rows, (cudaStream_t)stream);
     return launched(e, "values_kernel launch");
 }
 

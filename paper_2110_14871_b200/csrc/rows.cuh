@@ -20,6 +20,13 @@ inline gdws_status_t launched(cudaError_t e, const char *what)
     return cuda_fail(e, what);
 }
 
+// An arrival, at a barrier of either block of a pair, that publishes nothing in memory: the tensor memory it gives back has been
+// read into registers.  (A releasing arrival waits until the warp's stores to y have been performed.)
+__device__ __forceinline__ void mbar_arrive_relaxed(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
 // A wait on arrivals from both blocks of a pair: acquire at cluster scope, bounded like the others.
 static __device__ __noinline__ void mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int *abort_flag, int *status, int code)
 {
