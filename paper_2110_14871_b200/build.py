@@ -11,6 +11,8 @@ CSRC = os.path.join(_HERE, "csrc")
 SOURCES = ["plan.cu", "plan_mem.cu", "f32.cu", "f32_tc.cu", "bf16.cu", "gdw_tc.cu", "pack.cu", "fused.cu", "fused_tc.cu", "fold.cu", "fold_split.cu", "api.cu", "static_ws.cu", "diag.cu", "rows.cu", "pointwise8.cu"]
 HEADERS = [os.path.join(CSRC, "gdws_internal.h"), os.path.join(CSRC, "sm100.cuh"), os.path.join(CSRC, "rows.cuh"), os.path.join(_ROOT, "include", "gdws.h")]
 LIB_PATH = os.path.join(_HERE, "libgdws.so")
+BINDING = os.path.join(CSRC, "rows_binding.cpp")      # the calls on rows for Python, against torch's headers
+BINDING_PATH = os.path.join(_HERE, "_rows.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
@@ -25,6 +27,22 @@ def _nvcc() -> str:
     return "nvcc"
 
 
+def build_binding(force: bool = False) -> str:
+    """Compile ``_rows.so`` (host code only) next to this file; returns its path."""
+    deps = [BINDING, os.path.join(_ROOT, "include", "gdws.h")]
+    if not force and os.path.exists(BINDING_PATH) and all(os.path.getmtime(d) <= os.path.getmtime(BINDING_PATH) for d in deps):
+        return BINDING_PATH
+    import sysconfig
+    import torch
+    home = os.path.dirname(torch.__file__)
+    tmp = BINDING_PATH + f".tmp{os.getpid()}"
+    subprocess.check_call(["g++", "-std=c++17", "-O2", "-shared", "-fPIC", "-fvisibility=hidden", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                           "-I", os.path.join(_ROOT, "include"), "-isystem", os.path.join(home, "include"), "-isystem", os.path.join(home, "include", "torch", "csrc", "api", "include"),
+                           "-isystem", sysconfig.get_paths()["include"], BINDING, "-o", tmp, "-L" + os.path.join(home, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"])
+    os.replace(tmp, BINDING_PATH)
+    return BINDING_PATH
+
+
 def is_stale() -> bool:
     if not os.path.exists(LIB_PATH):
         return True
@@ -34,7 +52,8 @@ def is_stale() -> bool:
 
 
 def build_library(force: bool = False, verbose: bool = False) -> str:
-    """Compile the CUDA sources into ``libgdws.so`` next to this file; returns its path."""
+    """Compile the CUDA sources into ``libgdws.so`` and the binding of the calls on rows next to this file; returns the library's path."""
+    build_binding(force)
     if not force and not is_stale():
         return LIB_PATH
     objdir = os.path.join(_HERE, "_build")

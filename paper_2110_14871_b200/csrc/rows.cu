@@ -527,6 +527,7 @@ cudaError_t launch_rows(const RowsParams &P, bool few, cudaStream_t st)
 {
     const int n = P.cols + (SHIFTED ? 7 : 0);
     if (few && n > 256) {
+        if (n > 1024 && n <= 2048) return launch_rows<T, 8, SHIFTED, 8, 256, NORM>(P, st);
         if (n <= 1024) return launch_rows<T, 8, SHIFTED, 8, 128, NORM>(P, st);
         if (n <= 4096) return launch_rows<T, 8, SHIFTED, 8, 512, NORM>(P, st);
     }
@@ -566,7 +567,7 @@ cudaError_t launch_typed(const RowsParams &P, int sms, cudaStream_t st)
     const int64_t unit = 16 / sizeof(T);
     auto whole = [&](const void *p, int64_t ld) { return !p || (!((uintptr_t)p & 15) && (P.rows == 1 || ld % unit == 0)); };
     auto alike = [&](const void *p, int64_t ld) { return !p || ((uintptr_t)p % 16 == (uintptr_t)P.x % 16 && (P.rows == 1 || (ld - P.ldx) % unit == 0)); };
-    const bool few = P.rows <= 2 * sms;
+    const bool few = (int64_t)P.rows * P.cols <= (int64_t)8 * 2048 * sms;        // 8 values a thread do not fill the chip
     if (whole(P.x, P.ldx) && whole(P.residual, P.ldr) && whole(P.total, P.ldt) && !((uintptr_t)P.q & 7) && (P.rows == 1 || P.ldq % 8 == 0))
         return launch_rows<T, false, NORM>(P, few, st);
     return P.cols > 64 && alike(P.residual, P.ldr) && alike(P.total, P.ldt) ? launch_rows<T, true, NORM>(P, few, st) : launch_single<T, NORM>(P, st);
@@ -601,9 +602,11 @@ __device__ __forceinline__ typename Steps<VEC>::word load_steps(const int8_t *ro
     typedef typename Steps<VEC>::word Word;
     const int off = ALIGNED ? 0 : (int)((uintptr_t)(row + c) % VEC);
     if ((ALIGNED || c >= 0) && c + VEC <= cols && off == 0) return *reinterpret_cast<const Word *>(row + c);
-    if (!ALIGNED && off && c >= off && c - off + 2 * VEC <= cols) {           // two aligned words of the row
-        const Word *a = reinterpret_cast<const Word *>(row + c - off);
-        return a[0] >> (8 * off) | a[1] << (8 * (VEC - off));
+    if constexpr (!ALIGNED) {
+        if (off && c >= off && c - off + 2 * VEC <= cols) {                   // two aligned words of the row
+            const Word *a = reinterpret_cast<const Word *>(row + c - off);
+            return a[0] >> (8 * off) | a[1] << (8 * (VEC - off));
+        }
     }
     Word w = 0;
 #pragma unroll
@@ -646,8 +649,15 @@ __global__ void __launch_bounds__(256) values_kernel(const __grid_constant__ Val
         int c;
         if (!piece(i, row, c)) break;
         float v[VEC];
+        // q + 128 in the low mantissa bits of 2^23: one byte permutation, and an exact subtraction for two values at a time
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) v[e] = (float)(int8_t)(q[i] >> (8 * e)) * s[i];
+        for (int e = 0; e < VEC; e += 2) {
+            const uint32_t w = (e < 4 ? (uint32_t)q[i] : (uint32_t)(q[i] >> (VEC == 8 ? 32 : 0))) ^ 0x80808080u;
+            v[e] = __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7550 + e % 4));
+            v[e + 1] = __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7551 + e % 4));
+            add2(v[e], v[e + 1], -8388736.f, -8388736.f);
+            mul2(v[e], v[e + 1], s[i], s[i]);
+        }
         store_vec<VEC>((T *)P.y + row * P.ldy, c, P.cols, (!SHIFTED || c >= 0) && c + VEC <= P.cols, v);
     }
 }

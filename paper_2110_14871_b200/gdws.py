@@ -373,47 +373,41 @@ class Plan:
 
 # ---- rows in 8 bits
 
-# The descriptors of a call lie one behind the other and are packed at once: three of gdws_rows_t, then two of gdws_rows8_t (of
-# which a call may use fewer).  A small call's time is that of these lines, so they ask a tensor for nothing twice.
-_ROWS, _ROWS8 = "Pqqii", "PPqqi4x"
-_QUANTIZE, _NORM, _PRODUCT = (struct.Struct("@" + f).pack_into for f in (_ROWS + _ROWS8, 3 * _ROWS + _ROWS8, _ROWS + 2 * _ROWS8))
-_ROWS_SIZE, _ROWS8_SIZE = ctypes.sizeof(Rows), ctypes.sizeof(Rows8)
-assert struct.calcsize("@" + _ROWS) == _ROWS_SIZE and struct.calcsize("@" + _ROWS8) == _ROWS8_SIZE
-
-
+# A small call's time is the host's.  Ordinary arguments therefore go through `_rows` (csrc/rows_binding.cpp), which fills the C
+# structures from the tensors itself; what it does not take comes back as -1 and goes through the checks below, one by one.
 class _Descriptors(threading.local):
-    """Memory for the descriptors of one call, filled anew each time; every host thread has its own."""
+    """Memory for the descriptors of one call; every host thread has its own."""
 
     def __init__(self):
-        self.buffer = ctypes.create_string_buffer(3 * _ROWS_SIZE + 2 * _ROWS8_SIZE)
-        at = ctypes.addressof(self.buffer)
-        r, r2 = at + _ROWS_SIZE, at + 2 * _ROWS_SIZE
-        self.quantize = (at, r)                                          # x or y, q
-        self.norm = (at, r, r2, r2 + _ROWS_SIZE)                         # x, residual, total, q
-        self.product = (at, r, r + _ROWS8_SIZE)                          # y, x, w
+        self.rows, self.rows8 = [Rows() for _ in range(3)], [Rows8() for _ in range(2)]
 
 
 _descriptors = _Descriptors()
-_rows_lib = None       # the library, once torch has initialised CUDA
-_get_device = _get_stream = None
+_rows = None           # the native binding, once torch has initialised CUDA
+_get_device = None
 _int8 = _float32 = None
 
 
 def _rows_setup():
-    """The library; on a host without a GPU the calls then refuse every tensor."""
-    global _rows_lib, _get_device, _get_stream, _int8, _float32
+    """Loads what the calls on rows need; on a host without a GPU they then refuse every tensor."""
+    global _rows, _get_device, _int8, _float32
     import torch
     L = lib()
     _dtype_code(torch.empty(0, dtype=torch.float32))
     _int8, _float32 = torch.int8, torch.float32
+    if not os.path.exists(os.path.join(_HERE, "_rows.so")):
+        raise FileNotFoundError("_rows.so is missing: build it with `python -m paper_2110_14871_b200.build`")
+    from . import _rows as native
     if not torch.cuda.is_available():
         _get_device = lambda: -1  # noqa: E731
-        return L
-    torch.cuda.init()
-    _get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-    _get_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
-    _rows_lib = L
-    return L
+    else:
+        torch.cuda.init()
+        _get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+        stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+        native.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.gdws_quantize_rows, L.gdws_norm_quantize_rows, L.gdws_dequantize_rows, L.gdws_pointwise8)),
+                    _get_device, stream_of)
+    _rows = native
+    return native
 
 
 def _not_on(t, name: str, device: int):
@@ -437,20 +431,23 @@ def _geometry(t, name: str, device: int):
     return t.data_ptr(), (t.numel() // cols if cols else 0), cols, cols
 
 
-def _values(t, name: str, device: int):
-    """The fields of gdws_rows_t."""
+def _values(d: Rows, t, name: str, device: int) -> int:
+    """Fills a gdws_rows_t; returns its address."""
     code = _dtypes.get(t.dtype)
     if code is None:
         raise TypeError(f"{name}: unsupported dtype {t.dtype}")
-    return *_geometry(t, name, device), code
+    d.ptr, d.rows, d.ld, d.cols = _geometry(t, name, device)
+    d.dtype = code
+    return ctypes.addressof(d)
 
 
-def _steps(q, scale, name: str, device: int):
-    """The fields of gdws_rows8_t."""
+def _steps(d: Rows8, q, scale, name: str, device: int) -> int:
+    """Fills a gdws_rows8_t; returns its address."""
     if q.dtype is not _int8:
         raise TypeError(f"{name} must be int8")
-    at, rows, ld, cols = _geometry(q, name, device)
-    return at, _vector(scale, name + "'s scales", rows, device), rows, ld, cols
+    d.q, d.rows, d.ld, d.cols = _geometry(q, name, device)
+    d.scale = _vector(scale, name + "'s scales", d.rows, device)
+    return ctypes.addressof(d)
 
 
 def _vector(t, name: str, n: int, device: int) -> int:
@@ -472,71 +469,67 @@ def empty_rows8(rows: int, cols: int, device="cuda"):
 
 def quantize_rows(x, q, scale, stream=None) -> None:
     """gdws_quantize_rows: rows of x (fp32 or bf16) to 8 bits in q (int8) with one fp32 scale each in `scale`."""
-    L = _rows_lib or _rows_setup()
-    device, d = _get_device(), _descriptors
-    _QUANTIZE(d.buffer, 0, *_values(x, "x", device), *_steps(q, scale, "q", device))
-    px, pq = d.quantize
-    st = L.gdws_quantize_rows(px, pq, _get_stream(device) if stream is None else _stream(stream))
+    native = _rows or _rows_setup()
+    st = native.quantize_rows(x, q, scale) if stream is None else -1
+    if st < 0:
+        device, d = _get_device(), _descriptors
+        st = lib().gdws_quantize_rows(_values(d.rows[0], x, "x", device), _steps(d.rows8[0], q, scale, "q", device), _stream(stream))
     if st:
         raise GdwsError(st, last_error())
 
 
-_NO_ROWS = (0, 0, 0, 0, 0)
-
-
 def norm_quantize_rows(x, q, scale, weight=None, eps: float = 1e-6, residual=None, total=None, stream=None) -> None:
     """gdws_norm_quantize_rows: h = x + residual (written to `total`), 8 bits of h * weight / sqrt(mean h^2 + eps) in q and scale."""
-    L = _rows_lib or _rows_setup()
-    device, d = _get_device(), _descriptors
-    _NORM(d.buffer, 0, *_values(x, "x", device), *(_NO_ROWS if residual is None else _values(residual, "residual", device)),
-          *(_NO_ROWS if total is None else _values(total, "total", device)), *_steps(q, scale, "q", device))
-    w = code = None
-    if weight is not None:
-        code = _dtypes.get(weight.dtype)
-        if code is None:
-            raise TypeError(f"weight: unsupported dtype {weight.dtype}")
-        if weight.get_device() != device:
-            raise _not_on(weight, "weight", device)
-        if weight.numel() != x.shape[-1] or not weight.is_contiguous():
-            raise ValueError(f"weight: expected {x.shape[-1]} values, one behind the other")
-        w = weight.data_ptr()
-    px, pr, pt, pq = d.norm
-    st = L.gdws_norm_quantize_rows(px, None if residual is None else pr, None if total is None else pt, w, code or 0, eps, pq,
-                                   _get_stream(device) if stream is None else _stream(stream))
+    native = _rows or _rows_setup()
+    st = native.norm_quantize_rows(x, q, scale, weight, eps, residual, total) if stream is None else -1
+    if st < 0:
+        device, d = _get_device(), _descriptors
+        w, code = None, F32
+        if weight is not None:
+            code = _dtypes.get(weight.dtype)
+            if code is None:
+                raise TypeError(f"weight: unsupported dtype {weight.dtype}")
+            if weight.get_device() != device:
+                raise _not_on(weight, "weight", device)
+            if weight.numel() != x.shape[-1] or not weight.is_contiguous():
+                raise ValueError(f"weight: expected {x.shape[-1]} values, one behind the other")
+            w = weight.data_ptr()
+        st = lib().gdws_norm_quantize_rows(_values(d.rows[0], x, "x", device), None if residual is None else _values(d.rows[1], residual, "residual", device),
+                                           None if total is None else _values(d.rows[2], total, "total", device), w, code, eps,
+                                           _steps(d.rows8[0], q, scale, "q", device), _stream(stream))
     if st:
         raise GdwsError(st, last_error())
 
 
 def dequantize_rows(q, scale, y, stream=None) -> None:
     """gdws_dequantize_rows: y = q * scale (y: fp32 or bf16)."""
-    L = _rows_lib or _rows_setup()
-    device, d = _get_device(), _descriptors
-    _QUANTIZE(d.buffer, 0, *_values(y, "y", device), *_steps(q, scale, "q", device))
-    py, pq = d.quantize
-    st = L.gdws_dequantize_rows(pq, py, _get_stream(device) if stream is None else _stream(stream))
+    native = _rows or _rows_setup()
+    st = native.dequantize_rows(q, scale, y) if stream is None else -1
+    if st < 0:
+        device, d = _get_device(), _descriptors
+        st = lib().gdws_dequantize_rows(_steps(d.rows8[0], q, scale, "q", device), _values(d.rows[0], y, "y", device), _stream(stream))
     if st:
         raise GdwsError(st, last_error())
 
 
 def pointwise8(q, scale, w, w_scale, y, bias=None, relu: bool = False, stream=None) -> None:
     """gdws_pointwise8: y = (q w^T) * w_scale * scale + bias for 8-bit rows q and 8-bit weights w [D][columns]; optionally ReLU."""
-    L = _rows_lib or _rows_setup()
-    device, d = _get_device(), _descriptors
-    _PRODUCT(d.buffer, 0, *_values(y, "y", device), *_steps(q, scale, "q", device), *_steps(w, w_scale, "w", device))
-    py, px, pw = d.product
-    st = L.gdws_pointwise8(px, pw, None if bias is None else _vector(bias, "bias", y.shape[-1], device), relu, py,
-                           _get_stream(device) if stream is None else _stream(stream))
+    native = _rows or _rows_setup()
+    st = native.pointwise8(q, scale, w, w_scale, y, bias, relu) if stream is None else -1
+    if st < 0:
+        device, d = _get_device(), _descriptors
+        px, pw, py = _steps(d.rows8[0], q, scale, "q", device), _steps(d.rows8[1], w, w_scale, "w", device), _values(d.rows[0], y, "y", device)
+        st = lib().gdws_pointwise8(px, pw, None if bias is None else _vector(bias, "bias", y.shape[-1], device), int(bool(relu)), py, _stream(stream))
     if st:
         raise GdwsError(st, last_error())
 
 
 def pointwise8_kernel(q, scale, w, w_scale, y) -> int:
     """gdws_pointwise8_kernel: KERNEL8_* that this call takes."""
-    L = _rows_lib or _rows_setup()
+    _rows or _rows_setup()
     device, d, kernel = _get_device(), _descriptors, ctypes.c_int()
-    _PRODUCT(d.buffer, 0, *_values(y, "y", device), *_steps(q, scale, "q", device), *_steps(w, w_scale, "w", device))
-    py, px, pw = d.product
-    _check(L.gdws_pointwise8_kernel(px, pw, py, ctypes.byref(kernel)))
+    px, pw, py = _steps(d.rows8[0], q, scale, "q", device), _steps(d.rows8[1], w, w_scale, "w", device), _values(d.rows[0], y, "y", device)
+    _check(lib().gdws_pointwise8_kernel(px, pw, py, ctypes.byref(kernel)))
     return kernel.value
 
 
