@@ -796,10 +796,11 @@ gdws_status_t gdws_rows_status(void)
     const gdws_status_t st = rows_device(&device, &sms);
     if (st != GDWS_OK) return st;
     int word = 0;
-    const int zero = 0;
+    void *at = nullptr;
     cudaError_t e = cudaDeviceSynchronize();
-    if (e == cudaSuccess) e = cudaMemcpyFromSymbol(&word, g_rows_status, sizeof(int));
-    if (e == cudaSuccess && word) e = cudaMemcpyToSymbol(g_rows_status, &zero, sizeof(int));
+    if (e == cudaSuccess) e = cudaGetSymbolAddress(&at, g_rows_status);
+    if (e == cudaSuccess) e = cudaMemcpy(&word, at, sizeof(int), cudaMemcpyDeviceToHost);
+    if (e == cudaSuccess && word) e = cudaMemset(at, 0, sizeof(int));
     if (e != cudaSuccess) return cuda_fail(e, "status read");
     if (word) return fail(GDWS_ERR_DEVICE_TIMEOUT, "a bounded wait inside a kernel expired (status word 0x%x)", word);
     return GDWS_OK;
