@@ -323,7 +323,8 @@ GDWS_API size_t gdws_static_scratch_bytes(void);
  * Element (r, c) of gdws_rows_t is ptr[r * ld + c], of gdws_rows8_t it stands for scale[r] * q[r * ld + c].  rows >= 0 (at most
  * 2^31 - 1; with 0 rows nothing is done and pointers may be NULL), cols >= 1, ld >= cols (not looked at for a single row).
  * Pointers need the alignment of their element type only, whatever the general rule says.  Nothing but the elements themselves is
- * read or written: neither what lies between cols and ld nor rows behind the last one.  Outputs must not overlap inputs or each
+ * written, and used: neither what lies between cols and ld nor rows behind the last one (an aligned 4-byte word that holds an
+ * element may be read as a whole).  Outputs must not overlap inputs or each
  * other except where noted; columns of one buffer that do not meet (same ld) are no overlap.
  */
 typedef struct {
@@ -374,7 +375,7 @@ GDWS_API gdws_status_t gdws_dequantize_rows(const gdws_rows8_t *q, const gdws_ro
  *   bias   DEVICE float[D] or NULL;  y   F32 or BF16, x->rows x D, written
  * The sums are exact (32-bit integers; cols <= 131071, else GDWS_ERR_UNSUPPORTED), then fp32 in the order written, the last
  * multiplication and the bias as one fused multiply-add, and one rounding to y's type.  NaN stays NaN through the ReLU.
- * Rows of x and w that start at multiples of 16 bytes (pointer and ld) run on the tensor cores, others on the ALUs.
+ * Rows of x and w that start at multiples of 16 bytes (pointer and ld) run several times faster than others.
  * Errors: as gdws_quantize_rows, GDWS_ERR_UNSUPPORTED.
  */
 GDWS_API gdws_status_t gdws_pointwise8(const gdws_rows8_t *x, const gdws_rows8_t *w, const float *bias, int relu,
@@ -383,10 +384,10 @@ GDWS_API gdws_status_t gdws_pointwise8(const gdws_rows8_t *x, const gdws_rows8_t
 /* The kernels of gdws_pointwise8. */
 typedef enum {
     GDWS_KERNEL8_NONE = 0,   /* no rows: nothing is launched                                          */
-    GDWS_KERNEL8_ALU = 1,    /* any alignment                                                         */
+    GDWS_KERNEL8_ANY = 1,    /* any alignment                                                         */
     GDWS_KERNEL8_SLICES = 2, /* tensor cores, few outputs: clusters share a tile's sum                */
     GDWS_KERNEL8_PAIRS = 3,  /* tensor cores, many outputs: pairs of SMs share 256 x 256 of them      */
-    GDWS_KERNEL8_FEW = 4     /* at most 8 rows: w read once, four-byte dot products                   */
+    GDWS_KERNEL8_FEW = 4     /* at most 8 rows, any alignment: w read once, four-byte dot products    */
 } gdws_kernel8_t;
 /* gdws_pointwise8_kernel -- the kernel that this call takes on the current device (a B200 where there is none).  Diagnostic, host only. */
 GDWS_API gdws_status_t gdws_pointwise8_kernel(const gdws_rows8_t *x, const gdws_rows8_t *w, const gdws_rows_t *y, int *kernel);

@@ -47,6 +47,10 @@ __device__ __forceinline__ float max_nan(float v, float floor)
     asm("max.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(floor));
     return v;
 }
+
+// Whether rows start at multiples of 16 bytes, as TMA and 16-byte loads need it.
+bool whole16(const int8_t *q, int64_t rows, int64_t ld) { return !((uintptr_t)q & 15) && (rows == 1 || ld % 16 == 0); }
+
 struct P8Params {
     const int8_t *x, *w;
     const float *xs, *ws, *bias;
@@ -58,68 +62,91 @@ struct P8Params {
 };
 
 // ------------------------------------------------------------------------------------------
-// Any alignment: 64 rows x 64 output channels a block, 64 bytes of the rows at a time through shared memory, products of four
-// bytes on the ALUs.
+// Any alignment: 64 rows x 64 output channels a block, 64 columns of the rows at a time through registers into shared memory, from
+// there by warp-wide products of 16 x 8 x 32 (four-byte dot products run at some 30 a clock and SM here: 4000 x 2001 -> 2000 510 us).
 // ------------------------------------------------------------------------------------------
-__device__ __forceinline__ int load4(const int8_t *row, int k, int K, bool words)
-{
-    if (words && k + 4 <= K) return *reinterpret_cast<const int *>(row + k);
-    int v = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (k + e < K) v |= (int)(uint8_t)row[k + e] << (8 * e);
-    return v;
-}
+__device__ __forceinline__ int dot16(const int4 &a, const int4 &b, int acc) { return __dp4a(a.w, b.w, __dp4a(a.z, b.z, __dp4a(a.y, b.y, __dp4a(a.x, b.x, acc)))); }
+// A row that starts anywhere, read by aligned words that hold at least one of its bytes.
+struct Bytes {
+    const uint32_t *first;
+    int last;                    // the last such word
+    uint32_t shift;
+    __device__ __forceinline__ Bytes() {}
+    __device__ __forceinline__ Bytes(const int8_t *row, int K)
+    {
+        const int off = (int)((uintptr_t)row & 3);
+        first = reinterpret_cast<const uint32_t *>(row - off);
+        last = (off + K - 1) / 4;
+        shift = 8u * (uint32_t)off;
+    }
+    // the two words around columns k to k + 3 (k a multiple of 4), put together when they are needed, so that many are on their way
+    // at once; what lies behind the last column is anything
+    __device__ __forceinline__ uint2 load(int k) const { return make_uint2(first[min(k / 4, last)], first[min(k / 4 + 1, last)]); }
+    __device__ __forceinline__ int join(uint2 v) const { return (int)__funnelshift_r(v.x, v.y, shift); }
+};
+// The first n of four bytes, zeros for the others (it suffices that one factor has them).
+__device__ __forceinline__ int first4(int v, int n) { return n >= 4 ? v : (n <= 0 ? 0 : v & ((1 << (8 * n)) - 1)); }
 
 template <typename Y>
-__global__ void __launch_bounds__(256) p8_alu_kernel(const __grid_constant__ P8Params P, int tiles_d)
+__global__ void __launch_bounds__(256) p8_any_kernel(const __grid_constant__ P8Params P, int tiles_d)
 {
     grid_launch_dependents();
     grid_dependency_wait();
-    __shared__ int xt[64][17], wt[64][17];
+    __shared__ int xt[64][20], wt[64][20];           // 16 words a row; pitch 20: eight rows' four words lie in 32 banks
     const int tile_r = (int)blockIdx.x / tiles_d, r0 = tile_r * 64, d0 = ((int)blockIdx.x - tile_r * tiles_d) * 64;
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    const bool xw = !(((uintptr_t)P.x | (uintptr_t)P.ldx) & 3), ww = !(((uintptr_t)P.w | (uintptr_t)P.ldw) & 3);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    // rows and channels behind the last repeat it: what comes of them is not stored
+    Bytes xr[4], wr[4];
+    uint2 xn[4], wn[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        xr[i] = Bytes(P.x + (int64_t)min(r0 + ty + 16 * i, P.rows - 1) * P.ldx, P.K);
+        wr[i] = Bytes(P.w + (int64_t)min(d0 + ty + 16 * i, P.D - 1) * P.ldw, P.K);
+    }
+    auto fetch = [&](int k0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            xn[i] = xr[i].load(k0 + 4 * tx);
+            wn[i] = wr[i].load(k0 + 4 * tx);
+        }
+    };
+    // a warp: 16 rows, 32 channels as four products of 8; lane l has the sums of rows l / 4 and l / 4 + 8, channels 2 (l % 4) and the next
+    const int m0 = (warp & 3) * 16 + lane / 4, n0 = (warp >> 2) * 32, kw = lane % 4;
     int acc[4][4] = {};
+    fetch(0);
     for (int k0 = 0; k0 < P.K; k0 += 64) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = ty + 16 * i;
-            xt[row][tx] = r0 + row < P.rows ? load4(P.x + (int64_t)(r0 + row) * P.ldx, k0 + 4 * tx, P.K, xw) : 0;
-            wt[row][tx] = d0 + row < P.D ? load4(P.w + (int64_t)(d0 + row) * P.ldw, k0 + 4 * tx, P.K, ww) : 0;
-        }
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            int a[4], b[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { a[i] = xt[ty + 16 * i][k]; b[i] = wt[tx + 16 * i][k]; }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = __dp4a(a[i], b[j], acc[i][j]);
-        }
+        for (int i = 0; i < 4; ++i) { xt[ty + 16 * i][tx] = first4(xr[i].join(xn[i]), P.K - k0 - 4 * tx); wt[ty + 16 * i][tx] = wr[i].join(wn[i]); }
         __syncthreads();
-    }
+        if (k0 + 64 < P.K) fetch(k0 + 64);               // under this piece's products
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int d = d0 + tx + 16 * j;
-        if (d >= P.D) continue;
-        const float ws = P.ws[d], bias = P.bias ? P.bias[d] : 0.f;
+        for (int k = 0; k < 16; k += 8) {
+            const int a0 = xt[m0][k + kw], a1 = xt[m0 + 8][k + kw], a2 = xt[m0][k + 4 + kw], a3 = xt[m0 + 8][k + 4 + kw];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = r0 + ty + 16 * i;
-            if (r < P.rows) store8((Y *)P.y + (int64_t)r * P.ldy + d, finish8(acc[i][j], ws, P.xs[r], bias, P.floor));
+            for (int n = 0; n < 4; ++n) {
+                const int b0 = wt[n0 + 8 * n + lane / 4][k + kw], b1 = wt[n0 + 8 * n + lane / 4][k + 4 + kw];
+                asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                    : "+r"(acc[n][0]), "+r"(acc[n][1]), "+r"(acc[n][2]), "+r"(acc[n][3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+            }
         }
     }
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int r = r0 + m0 + (e >> 1) * 8, d = d0 + n0 + 8 * n + 2 * kw + (e & 1);
+            if (r < P.rows && d < P.D) store8((Y *)P.y + (int64_t)r * P.ldy + d, finish8(acc[n][e], P.ws[d], P.xs[r], P.bias ? P.bias[d] : 0.f, P.floor));
+        }
 }
 
-gdws_status_t p8_alu(const P8Params &P, cudaStream_t st)
+gdws_status_t p8_any(const P8Params &P, cudaStream_t st)
 {
     const int64_t tiles_d = ((int64_t)P.D + 63) / 64, tiles = ((int64_t)P.rows + 63) / 64 * tiles_d;
     if (tiles > 0x7fffffff) return fail(GDWS_ERR_UNSUPPORTED, "gdws_pointwise8: %d x %d outputs are more than one launch covers", P.rows, P.D);
-    const cudaError_t e = launch_overlapped(P.out_f32 ? p8_alu_kernel<float> : p8_alu_kernel<__nv_bfloat16>, dim3((unsigned)tiles), 256u, 0, st, P, (int)tiles_d);
-    return launched(e, "p8_alu_kernel launch");
+    const cudaError_t e = launch_overlapped(P.out_f32 ? p8_any_kernel<float> : p8_any_kernel<__nv_bfloat16>, dim3((unsigned)tiles), 256u, 0, st, P, (int)tiles_d);
+    return launched(e, "p8_any_kernel launch");
 }
 
 // ------------------------------------------------------------------------------------------
@@ -136,9 +163,9 @@ __device__ __forceinline__ int4 load_weights(const int8_t *p)
     asm volatile("ld.global.nc.L1::no_allocate.L2::256B.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
-__device__ __forceinline__ int dot16(const int4 &a, const int4 &b, int acc) { return __dp4a(a.w, b.w, __dp4a(a.z, b.z, __dp4a(a.y, b.y, __dp4a(a.x, b.x, acc)))); }
 
-template <typename Y, int R>
+// WHOLE: rows start at multiples of 16 bytes; otherwise the lanes take four columns each.
+template <typename Y, int R, bool WHOLE>
 __global__ void __launch_bounds__(256) p8_few_kernel(const __grid_constant__ P8Params P, int share)
 {
     grid_launch_dependents();
@@ -160,28 +187,57 @@ __global__ void __launch_bounds__(256) p8_few_kernel(const __grid_constant__ P8P
     const bool mine = me == 0 && lane < kSums && my_d < P.D && my_r < P.rows;
     const float ws = mine ? P.ws[my_d] : 0.f, xs = mine ? P.xs[my_r] : 0.f, bias = mine && P.bias ? P.bias[my_d] : 0.f;
     int acc[kFewD][R] = {};
-    const int whole = P.K & ~15;
-    constexpr int kAhead = R <= 2 ? 4 : 2;                                   // pieces in flight
-    for (int k = (me * 32 + lane) * 16; k < whole; k += kAhead * share * 512) {
-        int4 a[kAhead][kFewD];
+    if constexpr (WHOLE) {
+        const int whole = P.K & ~15;
+        constexpr int kAhead = R <= 2 ? 4 : 2;                                   // pieces in flight
+        for (int k = (me * 32 + lane) * 16; k < whole; k += kAhead * share * 512) {
+            int4 a[kAhead][kFewD];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i)
+            for (int i = 0; i < kAhead; ++i)
 #pragma unroll
-            for (int c = 0; c < kFewD; ++c) a[i][c] = k + i * share * 512 < whole ? load_weights(w[c] + k + i * share * 512) : make_int4(0, 0, 0, 0);
+                for (int c = 0; c < kFewD; ++c) a[i][c] = k + i * share * 512 < whole ? load_weights(w[c] + k + i * share * 512) : make_int4(0, 0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i)
+            for (int i = 0; i < kAhead; ++i)
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const int4 b = k + i * share * 512 < whole ? __ldg(reinterpret_cast<const int4 *>(x[r] + k + i * share * 512)) : make_int4(0, 0, 0, 0);
+                for (int r = 0; r < R; ++r) {
+                    const int4 b = k + i * share * 512 < whole ? __ldg(reinterpret_cast<const int4 *>(x[r] + k + i * share * 512)) : make_int4(0, 0, 0, 0);
 #pragma unroll
-                for (int c = 0; c < kFewD; ++c) acc[c][r] = dot16(a[i][c], b, acc[c][r]);
+                    for (int c = 0; c < kFewD; ++c) acc[c][r] = dot16(a[i][c], b, acc[c][r]);
+                }
+        }
+        if (me == 0 && lane < P.K - whole) {                                     // the last columns, one by one
+#pragma unroll
+            for (int c = 0; c < kFewD; ++c)
+#pragma unroll
+                for (int r = 0; r < R; ++r) acc[c][r] += (int)w[c][whole + lane] * (int)x[r][whole + lane];
+        }
+    } else {
+        constexpr int kAhead = R <= 2 ? 8 : 4;
+        Bytes wb[kFewD], xb[R];
+#pragma unroll
+        for (int c = 0; c < kFewD; ++c) wb[c] = Bytes(w[c], P.K);
+#pragma unroll
+        for (int r = 0; r < R; ++r) xb[r] = Bytes(x[r], P.K);
+        for (int k0 = (me * 32 + lane) * 4; k0 < P.K; k0 += kAhead * share * 128) {
+            uint2 a[kAhead][kFewD];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+                for (int c = 0; c < kFewD; ++c) a[i][c] = wb[c].load(k0 + i * share * 128);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int k = k0 + i * share * 128;
+                int v[kFewD];
+#pragma unroll
+                for (int c = 0; c < kFewD; ++c) v[c] = wb[c].join(a[i][c]);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const int u = first4(xb[r].join(xb[r].load(k)), P.K - k);
+#pragma unroll
+                    for (int c = 0; c < kFewD; ++c) acc[c][r] = __dp4a(v[c], u, acc[c][r]);
+                }
             }
-    }
-    if (me == 0 && lane < P.K - whole) {                                     // the last columns, one by one
-#pragma unroll
-        for (int c = 0; c < kFewD; ++c)
-#pragma unroll
-            for (int r = 0; r < R; ++r) acc[c][r] += (int)w[c][whole + lane] * (int)x[r][whole + lane];
+        }
     }
     int sum = 0;
 #pragma unroll
@@ -200,17 +256,20 @@ __global__ void __launch_bounds__(256) p8_few_kernel(const __grid_constant__ P8P
     if (mine) store8((Y *)P.y + (int64_t)my_r * P.ldy + my_d, finish8(sum, ws, xs, bias, P.floor));
 }
 
-template <typename Y>
+template <typename Y, bool WHOLE>
 cudaError_t launch_few(const P8Params &P, unsigned blocks, int share, cudaStream_t st)
 {
-    auto kernel = P.rows == 1 ? p8_few_kernel<Y, 1> : P.rows == 2 ? p8_few_kernel<Y, 2> : P.rows <= 4 ? p8_few_kernel<Y, 4> : p8_few_kernel<Y, 8>;
+    auto kernel = P.rows == 1 ? p8_few_kernel<Y, 1, WHOLE> : P.rows == 2 ? p8_few_kernel<Y, 2, WHOLE> : P.rows <= 4 ? p8_few_kernel<Y, 4, WHOLE> : p8_few_kernel<Y, 8, WHOLE>;
     return launch_overlapped(kernel, dim3(blocks), 256u, 0, st, P, share);
 }
 gdws_status_t p8_few(const P8Params &P, int share, cudaStream_t st)
 {
     const int64_t groups = ((int64_t)P.D + kFewD - 1) / kFewD;
     const unsigned blocks = (unsigned)((groups * share + 7) / 8);
-    return launched(P.out_f32 ? launch_few<float>(P, blocks, share, st) : launch_few<__nv_bfloat16>(P, blocks, share, st), "p8_few_kernel launch");
+    const bool whole = whole16(P.x, P.rows, P.ldx) && whole16(P.w, P.D, P.ldw);
+    const cudaError_t e = P.out_f32 ? (whole ? launch_few<float, true>(P, blocks, share, st) : launch_few<float, false>(P, blocks, share, st))
+                                    : (whole ? launch_few<__nv_bfloat16, true>(P, blocks, share, st) : launch_few<__nv_bfloat16, false>(P, blocks, share, st));
+    return launched(e, "p8_few_kernel launch");
 }
 
 // ------------------------------------------------------------------------------------------
@@ -607,7 +666,7 @@ gdws_status_t rows_map(CUtensorMap *map, const int8_t *q, int64_t rows, int cols
 }
 
 struct P8Choice {
-    int kernel = GDWS_KERNEL8_ALU;
+    int kernel = GDWS_KERNEL8_ANY;
     int nt = 0, split = 1;       // slices: rows of a tile, blocks of a cluster; few rows: warps that share a group's columns (split)
 };
 
@@ -620,8 +679,6 @@ int slices_stages(const P8Choice &c, int pieces)
     return mine <= most ? mine : most / kP8Loaders * kP8Loaders;
 }
 
-// Whether TMA can read these rows.
-bool whole16(const int8_t *q, int64_t rows, int64_t ld) { return !((uintptr_t)q & 15) && (rows == 1 || ld % 16 == 0); }
 
 // Estimated times in us, of calls on data in L2, fitted to 250 timings of 40 sizes on a B200 (most within 15 %).
 //
@@ -661,11 +718,11 @@ double pairs_us(const P8Params &P, int sms)
 P8Choice p8_choose(const P8Params &P, int sms, const int *clusters)
 {
     P8Choice best;
-    if (!whole16(P.x, P.rows, P.ldx) || !whole16(P.w, P.D, P.ldw)) return best;
+    const bool whole = whole16(P.x, P.rows, P.ldx) && whole16(P.w, P.D, P.ldw);
     const int pieces = (P.K + kPiece - 1) / kPiece;
+    double us = 1e9;
     // (the pairs' kernel keeps the distance of y's rows in 32 bits)
-    best.kernel = P.ldy < 0x1fffffff ? GDWS_KERNEL8_PAIRS : GDWS_KERNEL8_ALU;
-    double us = best.kernel == GDWS_KERNEL8_PAIRS ? pairs_us(P, sms) : 1e9;
+    if (whole && P.ldy < 0x1fffffff) { best.kernel = GDWS_KERNEL8_PAIRS; us = pairs_us(P, sms); }
     if (P.rows <= kFewRows && few_us(P) < us) {
         us = few_us(P);
         best.kernel = GDWS_KERNEL8_FEW;
@@ -675,6 +732,7 @@ P8Choice p8_choose(const P8Params &P, int sms, const int *clusters)
         if (P.rows <= 4) while (best.split < 8 && groups * best.split < 16 * sms && best.split * 512 < P.K) best.split *= 2;
         else if (groups * 2 <= 16 * sms && P.K > 512) best.split = 2;
     }
+    if (!whole) return best;
     for (int nt = 16; nt <= 128; nt *= 2) {
         for (int split = 1; split <= std::min(8, pieces); split *= 2) {
             P8Choice c;
@@ -770,7 +828,7 @@ gdws_status_t gdws_pointwise8(const gdws_rows8_t *x, const gdws_rows8_t *w, cons
     cluster_capacities(device, sms, clusters);
     const P8Choice c = p8_choose(P, sms, clusters);
     if (c.kernel == GDWS_KERNEL8_FEW) return p8_few(P, c.split, (cudaStream_t)stream);
-    return c.kernel == GDWS_KERNEL8_ALU ? p8_alu(P, (cudaStream_t)stream) : p8_tc(P, c, device, sms, (cudaStream_t)stream);
+    return c.kernel == GDWS_KERNEL8_ANY ? p8_any(P, (cudaStream_t)stream) : p8_tc(P, c, device, sms, (cudaStream_t)stream);
 }
 
 gdws_status_t gdws_pointwise8_kernel(const gdws_rows8_t *x, const gdws_rows8_t *w, const gdws_rows_t *y, int *kernel)

@@ -26,7 +26,7 @@ OPT_PATH, OPT_RELU, OPT_TILE, OPT_A_LAYOUT, OPT_DW_MATH, OPT_OUT_DTYPE = range(6
 PATH_AUTO, PATH_FUSED, PATH_UNFUSED = 0, 1, 2
 (KERNEL_TWO_STAGES_ALU, KERNEL_TWO_STAGES_TC, KERNEL_FOLDED_PAIRS, KERNEL_FOLDED_SLICES, KERNEL_F32_ALU, KERNEL_F32_PIECES,
  KERNEL_GDW_ALU, KERNEL_GDW_TC) = range(1, 9)
-KERNEL8_NONE, KERNEL8_ALU, KERNEL8_SLICES, KERNEL8_PAIRS, KERNEL8_FEW = range(5)
+KERNEL8_NONE, KERNEL8_ANY, KERNEL8_SLICES, KERNEL8_PAIRS, KERNEL8_FEW = range(5)
 
 EXPORTS = [
     "gdws_plan", "gdws_plan_set_option", "gdws_plan_info", "gdws_plan_tables", "gdws_plan_tile",
