@@ -44,8 +44,8 @@ Extent vector_of(const void *p, int64_t bytes) { return {(uintptr_t)p, 1, bytes,
 
 gdws_status_t check_shape(const char *call, const char *name, int64_t rows, int64_t cols, int64_t ld)
 {
-    if (rows < 0 || rows > 0x7fffffff) return fail(GDWS_ERR_INVALID_ARG, "%s: %s->rows=%lld is outside 0..2^31-1", call, name, (long long)rows);
-    if (cols < 1) return fail(GDWS_ERR_INVALID_ARG, "%s: %s->cols must be >= 1 (got %lld)", call, name, (long long)cols);
+    if (rows < 0 || rows > kMostRows) return fail(GDWS_ERR_INVALID_ARG, "%s: %s->rows=%lld is outside 0..2^31-1024", call, name, (long long)rows);
+    if (cols < 1 || cols > kMostCols) return fail(GDWS_ERR_INVALID_ARG, "%s: %s->cols=%lld is outside 1..2^30", call, name, (long long)cols);
     if (rows > 1 && (ld < cols || ld > ((int64_t)1 << 40) / 4)) return fail(GDWS_ERR_INVALID_ARG, "%s: %s->ld=%lld does not fit rows of %lld", call, name, (long long)ld, (long long)cols);
     return GDWS_OK;
 }

@@ -5,6 +5,7 @@
 
 namespace gdws {
 
+constexpr int kMostRows = 0x7fffffff - 1023, kMostCols = 1 << 30;      // so that 32-bit indexes may go a tile too far
 constexpr int kMost8 = 131071;      // products of two 8-bit integers whose sum fits 32 bits: 131071 * 2^14 < 2^31
 
 gdws_status_t check_rows(const char *call, const char *name, const gdws_rows_t *m);

@@ -424,6 +424,8 @@ def _geometry(t, name: str, device: int):
         ld, one = t.stride()
         if one != 1 and cols > 1:
             raise ValueError(f"{name}: the elements of a row must lie one behind the other")
+        if cols >= 1 << 31:
+            raise ValueError(f"{name}: rows of {cols} values are too long")
         return t.data_ptr(), rows, ld, cols
     if len(shape) < 2 or not t.is_contiguous():
         raise ValueError(f"{name}: expected two dimensions, or more in a contiguous tensor (an NHWC map)")

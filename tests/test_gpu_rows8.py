@@ -1,5 +1,9 @@
 """gdws_quantize_rows, gdws_norm_quantize_rows and gdws_dequantize_rows against their definitions in 64 bits: every q equal, sums
 of squares within the rounding of their fp32 additions, nothing written beside the rows."""
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
@@ -86,6 +90,27 @@ def test_norm_quantize(rows, cols, gap, shift, dtype, residual, total, weight):
             f.check("a matrix")
 
 
+@pytest.mark.parametrize("cols", [5, 61, 130, 1000, 1333, 5003, 20001])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_matrices_that_lie_differently(dtype, cols):
+    """x, residual and total each at another place within 16 bytes, the weight off its boundary, q at every place."""
+    x, r = values(5, cols, dtype, cols), values(5, cols, dtype, cols + 1)
+    w = Field(1, cols, torch.float32, None, 1)
+    w.t.copy_(1 + 0.2 * values(1, cols, "f32", 3))
+    for sx, sr, st in ((0, 1, 2), (3, 3, 3), (1, 1, 1)):
+        fx, fr, ft, scale = field_of(x, cols + 1, sx), field_of(r, cols + (1 if sx == sr else 2), sr), Field(5, cols, TYPES[dtype], cols + 1, st), Field(1, 5, torch.float32)
+        for sq in range(8):
+            q = Field(5, cols, torch.int8, cols + sq, sq)
+            gdws.norm_quantize_rows(fx.t, q.t, scale.t[0], weight=w.t[0], residual=fr.t, total=ft.t)
+            h = x.float() + r.float()
+            assert torch.equal(q.t, steps_of(h * w.t)[0]) and torch.equal(ft.t, h.to(TYPES[dtype]))
+            y = Field(5, cols, TYPES[dtype], cols + 3, sq)
+            gdws.dequantize_rows(q.t, scale.t[0], y.t)
+            assert torch.equal(y.t, (q.t.float() * scale.t[0][:, None]).to(TYPES[dtype]))
+            for f in (fx, fr, ft, q, y, scale, w):
+                f.check("a matrix")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_halfway_cases(dtype):
     """Quotients that lie exactly between two integers, and next to it."""
@@ -151,6 +176,49 @@ def test_no_rows_and_views():
     q, scale = gdws.empty_rows8(30, 24)
     gdws.norm_quantize_rows(both[:, :24], q, scale, total=both[:, 24:])
     assert torch.equal(both[:, 24:], x) and torch.equal(q, qa.view(30, 24))
+
+
+def test_binding_says_what_is_wrong():
+    x = values(4, 64, "bf16", 1)
+    q, scale = gdws.empty_rows8(4, 64)
+    y = torch.empty((4, 64), device="cuda")
+    cpu = torch.zeros((4, 64))
+    for error, run in [(ValueError, lambda: gdws.quantize_rows(cpu, q, scale)), (ValueError, lambda: gdws.quantize_rows(x, q.cpu(), scale)), (ValueError, lambda: gdws.quantize_rows(x, q, scale.cpu())),
+                       (TypeError, lambda: gdws.quantize_rows(x.half(), q, scale)), (TypeError, lambda: gdws.quantize_rows(x, q.to(torch.uint8), scale)), (TypeError, lambda: gdws.quantize_rows(x, q, scale.double())),
+                       (ValueError, lambda: gdws.quantize_rows(x, q, scale[:3])), (ValueError, lambda: gdws.quantize_rows(x, q, torch.zeros(8, device="cuda")[::2])), (ValueError, lambda: gdws.quantize_rows(x.t(), q, scale)),
+                       (gdws.GdwsError, lambda: gdws.quantize_rows(x[:, :60], q, scale)), (gdws.GdwsError, lambda: gdws.quantize_rows(x.expand(4, 64)[:1].expand(4, 64), q, scale)),
+                       (ValueError, lambda: gdws.norm_quantize_rows(x, q, scale, weight=torch.ones(63, device="cuda"))), (TypeError, lambda: gdws.norm_quantize_rows(x, q, scale, weight=torch.ones(64, device="cuda").half())),
+                       (gdws.GdwsError, lambda: gdws.norm_quantize_rows(x, q, scale, residual=x.float())), (gdws.GdwsError, lambda: gdws.norm_quantize_rows(x, q, scale, eps=0.0)),
+                       (gdws.GdwsError, lambda: gdws.dequantize_rows(q, scale, y[:3])), (ValueError, lambda: gdws.pointwise8(q, scale, q, scale, torch.empty((4, 4), device="cuda"), bias=torch.zeros(5, device="cuda")))]:
+        with pytest.raises(error):
+            run()
+    gdws.norm_quantize_rows(x, q, scale, eps=1)          # any number will do
+
+
+FIRST_CALL = """
+import torch
+from paper_2110_14871_b200 import gdws
+x = torch.arange(64 * 520, device="cuda").remainder(97).float().view(64, 520)
+q, scale = gdws.empty_rows8(64, 520)
+y, z = torch.empty((64, 64), device="cuda"), torch.empty((64, 520), dtype=torch.bfloat16, device="cuda")
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    gdws.norm_quantize_rows(x, q, scale)
+    gdws.pointwise8(q, scale, q, scale, y)
+    gdws.dequantize_rows(q, scale, z)
+g.replay()
+torch.cuda.synchronize()
+gdws.rows_status()
+v = q.double() * scale.double()[:, None]
+assert (y.double() - v @ v.t()).abs().max() < 1e-4 * y.abs().max() and q.any()
+print("ok")
+"""
+
+
+def test_the_first_call_of_a_process_may_be_captured():
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALL], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout == "ok\n", r.stderr[-2000:]
 
 
 def test_streams_graphs_and_the_same_result_twice():

@@ -28,8 +28,8 @@ def call(name, *args):
     return getattr(gdws.lib(), name)(*refs)
 
 
-BAD_ROWS = [dict(ptr=None), dict(ptr=BASE + 1), dict(n=-1), dict(n=1 << 31), dict(cols=0), dict(cols=-3), dict(ld=63), dict(ld=-64), dict(dtype=2), dict(dtype=gdws.F32, ptr=BASE + 2)]
-BAD_ROWS8 = [dict(q=None), dict(scale=None), dict(scale=BASE * 3 + 2), dict(n=-1), dict(cols=0), dict(ld=63)]
+BAD_ROWS = [dict(ptr=None), dict(ptr=BASE + 1), dict(n=-1), dict(n=1 << 31), dict(n=(1 << 31) - 1023), dict(cols=0), dict(cols=-3), dict(cols=(1 << 30) + 1, ld=1 << 31), dict(ld=63), dict(ld=-64), dict(dtype=2), dict(dtype=gdws.F32, ptr=BASE + 2)]
+BAD_ROWS8 = [dict(q=None), dict(scale=None), dict(scale=BASE * 3 + 2), dict(n=-1), dict(n=(1 << 31) - 1023), dict(cols=0), dict(cols=(1 << 30) + 1, ld=1 << 31), dict(ld=63)]
 
 
 @pytest.mark.parametrize("bad", BAD_ROWS)
@@ -97,6 +97,24 @@ def test_overlaps():
         assert call("gdws_pointwise8", rows8(), w, BASE * 7, 0, rows(ptr, cols=6), None) == gdws.ERR_INVALID_ARG and "overlap" in gdws.last_error()
     # columns of one buffer
     assert call("gdws_norm_quantize_rows", rows(ld=128), None, rows(BASE + 126, ld=128), None, 0, 1e-6, rows8(), None) == gdws.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("rows_,K,D,kernel", [
+    (1, 4096, 4096, gdws.KERNEL8_FEW), (8, 512, 64, gdws.KERNEL8_FEW), (9, 512, 64, gdws.KERNEL8_SLICES), (16, 4096, 16384, gdws.KERNEL8_SLICES), (128, 1280, 256, gdws.KERNEL8_SLICES),
+    (16384, 1280, 256, gdws.KERNEL8_PAIRS), (4096, 4096, 4096, gdws.KERNEL8_PAIRS), (0, 64, 64, gdws.KERNEL8_NONE)])
+def test_kernel_of_a_call(rows_, K, D, kernel):
+    """As a B200 chooses, by estimated time; rows that start anywhere do not go through TMA."""
+    def choice(x, w, y):
+        k = ctypes.c_int(-1)
+        assert call("gdws_pointwise8_kernel", x, w, y, ctypes.byref(k)) == gdws.OK
+        return k.value
+
+    x, w, y = rows8(BASE, BASE * 3, rows_, K, K), rows8(BASE * 4, BASE * 5, D, K, K), rows(BASE * 6, rows_, D, D)
+    assert choice(x, w, y) == kernel
+    other = kernel if kernel in (gdws.KERNEL8_FEW, gdws.KERNEL8_NONE) else gdws.KERNEL8_ANY
+    assert choice(rows8(BASE + 4, BASE * 3, rows_, K, K), w, y) == other
+    assert choice(x, rows8(BASE * 4, BASE * 5, D, K + 1, K), y) == other
+    assert call("gdws_pointwise8_kernel", x, w, y, None) == gdws.ERR_INVALID_ARG
 
 
 def test_binding_refuses_what_is_not_on_the_current_device():
