@@ -211,10 +211,12 @@ __device__ __forceinline__ float lifted(float &m)
     m *= lift;
     return lift;
 }
-// q, the integer that t was rounded to, or its neighbour; d = t minus that integer.
-__device__ __forceinline__ int exact_step(float u, float m, float t, float d, int q)
+// The integer in r = t + kMagic or its neighbour towards t; d = t - (r - kMagic), some half.  (q comes from the very r that d comes
+// from: the compiler may form u * inv + kMagic in one rounding in one place and in two in another.)
+__device__ __forceinline__ int exact_step(float u, float m, float r, float d)
 {
-    const float s = copysignf(1.f, d), k = fmaf(2.f, t - d, s) * 0x1p-8f;
+    const int q = __float_as_int(r);
+    const float s = copysignf(1.f, d), k = fmaf(2.f, r - kMagic, s) * 0x1p-8f;
     const float a = u * (254.f / 256.f), a2 = fmaf(u, 254.f / 256.f, -a);
     const float past = (fmaf(-k, m, a) + a2) * s;          // how far the quotient lies beyond the middle
     return past > 0.f || (past == 0.f && (q & 1)) ? q + (int)s : q;
@@ -249,9 +251,30 @@ __device__ __forceinline__ void quantize(const float (&u)[N], float m, float inv
     if (far > kNear) {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const float d = t[e] - ((t[e] + kMagic) - kMagic);
-            if (fabsf(d) > kNear) q[e] = exact_step(u[e], m, t[e], d, q[e]);
+            const float r = t[e] + kMagic, d = t[e] - (r - kMagic);
+            if (fabsf(d) > kNear) q[e] = exact_step(u[e], m, r, d);
         }
+    }
+}
+// The same for bf16 numbers u and m, where a third of the warps would have an element to decide about.  With 8-bit significands the
+// quotient lies exactly in the middle or at least 1 / (254 * 255) = 1.5e-5 of itself away from it.  t is off by 1.2e-7 of itself, so
+// rounding it to 17 bits (2^-18, by Veltkamp's splitting: c = (2^7 + 1) t, c - (c - t)) moves it onto the middle if it belongs
+// there and not across it otherwise; the addition of kMagic then rounds as it should.
+__device__ __forceinline__ void quantize_short(const float (&u)[8], float inv, int (&q)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        float t0 = u[e], t1 = u[e + 1];
+        mul2(t0, t1, inv, inv);
+        float c0 = t0, c1 = t1;
+        mul2(c0, c1, 128.f, 128.f);          // exact, so that a fused multiply-add makes no difference
+        add2(c0, c1, t0, t1);
+        float d0 = c0, d1 = c1;
+        add2(d0, d1, -t0, -t1);
+        add2(c0, c1, -d0, -d1);
+        add2(c0, c1, kMagic, kMagic);
+        q[e] = __float_as_int(c0);
+        q[e + 1] = __float_as_int(c1);
     }
 }
 template <int VEC>
@@ -433,11 +456,22 @@ __global__ void __launch_bounds__(TPR < 64 ? 128 : TPR) rows8_kernel(const __gri
     const int by = SHIFTED ? (int)((8 - ((uintptr_t)qrow - (uintptr_t)shift) % 8) % 8) : 0;      // from q's vectors to its next boundary of 8 bytes
     auto column = [&](int i) { return (t + i * TPR) * VEC - shift; };
     auto whole = [&](int c) { return VEC > 1 && (!SHIFTED || c >= 0) && c + VEC <= P.cols; };
-    float u[N], most = 0.f, squares[2] = {};
-    {
-        Piece<T, VEC, NORM> p[kPieces];
+    // bf16 values that nothing is added to stay as they are, two to a register: half of the registers, more rows at a time
+    constexpr bool kPacked = !NORM && VEC == 8 && sizeof(T) == 2;
+    float u[kPacked ? 1 : N], most = 0.f, squares[2] = {};
+    Piece<T, VEC, NORM> p[kPieces];
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) p[i].load(P, r, column(i), whole(column(i)));
+    for (int i = 0; i < kPieces; ++i) p[i].load(P, r, column(i), whole(column(i)));
+    if constexpr (kPacked) {
+        uint32_t most2 = 0;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const uint32_t w[4] = {p[i].x.w[0].x, p[i].x.w[0].y, p[i].x.w[0].z, p[i].x.w[0].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(most2) : "r"(w[e] & 0x7fff7fffu));
+        }
+        most = larger(__uint_as_float(most2 << 16), __uint_as_float(most2 & 0xffff0000u));
+    } else {
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
             const int c = column(i);
@@ -452,17 +486,22 @@ __global__ void __launch_bounds__(TPR < 64 ? 128 : TPR) rows8_kernel(const __gri
     const bool fine = finite_row<NORM>(top, squares[0]);
     float m = fine ? __uint_as_float(top) : 0.f;
     const float lift = lifted(m), inv = m > 0.f ? 127.f / m : 0.f;
-    if (lift != 1.f || !fine) {
-#pragma unroll
-        for (int e = 0; e < N; ++e) u[e] = fine ? u[e] * lift : 0.f;
-    }
+    const bool odd = lift != 1.f || !fine;
 #pragma unroll
     for (int g = 0; g < N; g += 8) {
         float v[8];
         int q[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = u[g + e];
-        quantize<8>(v, m, inv, q);
+        for (int e = 0; e < 8; ++e) {
+            if constexpr (kPacked) v[e] = to_float(p[g / VEC].x.e[e]);
+            else v[e] = u[g + e];
+        }
+        if (odd) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = fine ? v[e] * lift : 0.f;
+        }
+        if constexpr (kPacked) quantize_short(v, inv, q);
+        else quantize<8>(v, m, inv, q);
         if constexpr (SHIFTED) {
             if (__any_sync(0xffffffffu, by != 0)) {          // a warp's rows may lie differently
                 const int c = column(g / VEC);

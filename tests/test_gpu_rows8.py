@@ -130,6 +130,35 @@ def test_halfway_cases(dtype):
     assert torch.equal(q, steps_of(x.float())[0])
 
 
+def test_every_pair_of_bf16_significands():
+    """127 u / m for all 8-bit significands of u and m and nine binades of u: ties and what lies nearest to them."""
+    u = torch.cat([torch.arange(128, 256, device="cuda").float() * 2.0 ** -k for k in range(9)])
+    for m in range(128, 256):
+        row = torch.cat([u[u <= m], torch.tensor([float(m)], device="cuda")])
+        x = torch.stack([row, -row, row * 2.0 ** 100, row * 2.0 ** -100, row * 2.0 ** -130]).bfloat16()
+        q, scale = gdws.empty_rows8(*x.shape)
+        for run in (gdws.quantize_rows, gdws.norm_quantize_rows):
+            if run is gdws.norm_quantize_rows:
+                x = x[[0, 1, 3, 4]].contiguous()                 # 2^100 squared passes fp32
+                q, scale = gdws.empty_rows8(*x.shape)
+            run(x, q, scale)
+            assert torch.equal(q, steps_of(x.float())[0]), m
+
+
+def test_neighbours_of_ties_in_fp32():
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    for ulps in range(-3, 4):
+        m = torch.rand((64, 1), generator=gen, device="cuda") * 2.0 ** torch.randint(-20, 20, (64, 1), generator=gen, device="cuda").float() + 1e-6
+        u = (torch.randint(0, 127, (64, 500), generator=gen, device="cuda").float() + 0.5) * m / 127
+        for _ in range(abs(ulps)):
+            u = torch.nextafter(u, torch.full_like(u, float("inf") if ulps > 0 else -float("inf")))
+        x = torch.cat([torch.minimum(u, m), -torch.minimum(u, m), m], 1)
+        q, scale = gdws.empty_rows8(*x.shape)
+        for run in (gdws.quantize_rows, gdws.norm_quantize_rows):
+            run(x, q, scale)
+            assert torch.equal(q, steps_of(x)[0])
+
+
 @pytest.mark.parametrize("cols", [5, 256, 1000, 4096, 40000])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_zero_tiny_huge_and_not_finite(dtype, cols):
