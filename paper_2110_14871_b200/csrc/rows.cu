@@ -157,20 +157,30 @@ union Raw {
     T e[VEC];
     __device__ __forceinline__ Raw() {}
 };
-// whole: all of them exist and lie on a boundary of 16 bytes.  Others are taken one by one; c may be negative.
-template <int VEC, typename T>
+// c may be negative.  whole: all of them exist and lie on a boundary of 16 bytes.  Others are taken one by one, or, where they are
+// known to lie on such a boundary (ALIGNED), as every piece that holds a value of the row, and what else it holds is set to zero.
+// (1000 x 10001, quantization: 21 us one by one, 13.5 by pieces.  With a residual and a weight to load it was slower by pieces, 8192
+// x 4096 46 -> 60 us, whatever the order of the conditions.)
+template <int VEC, bool ALIGNED, typename T>
 __device__ __forceinline__ void load_raw(const T *row, int c, int cols, bool whole, Raw<VEC, T> &b)
 {
     if constexpr (VEC == 1) {
         from_float(0.f, b.e[0]);
         if (c < cols) b.e[0] = row[c];
     } else {
-        constexpr int kPieces = (int)(VEC * sizeof(T) / 16);
+        constexpr int kPieces = (int)(VEC * sizeof(T) / 16), kPer = 16 / (int)sizeof(T);
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) b.w[i] = make_uint4(0, 0, 0, 0);
         if (whole) {
 #pragma unroll
             for (int i = 0; i < kPieces; ++i) b.w[i] = reinterpret_cast<const uint4 *>(row + c)[i];
+        } else if constexpr (ALIGNED) {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i)
+                if (c + kPer * (i + 1) > 0 && c + kPer * i < cols) b.w[i] = reinterpret_cast<const uint4 *>(row + c)[i];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                if ((unsigned)(c + e) >= (unsigned)cols) from_float(0.f, b.e[e]);
         } else {
 #pragma unroll
             for (int e = 0; e < VEC; ++e)
@@ -334,15 +344,16 @@ __device__ __forceinline__ void reduce_row(uint32_t &most, float &squares)
         for (int o = kLanes / 2; o; o >>= 1) squares += __shfl_xor_sync(0xffffffffu, squares, o);
     }
     if constexpr (TPR > 32) {
-        constexpr int kWarps = TPR / 32;
-        __shared__ uint32_t most_of[kWarps];
-        __shared__ float squares_of[kWarps];
+        constexpr int kWarps = TPR / 32, kAll = TPR < 128 ? 4 : kWarps;      // of a row, of the block
+        __shared__ uint32_t most_of[kAll];
+        __shared__ float squares_of[kAll];
         const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
         if (lane == 0) { most_of[warp] = most; squares_of[warp] = squares; }
         __syncthreads();
-        most = __reduce_max_sync(0xffffffffu, most_of[lane & (kWarps - 1)]);
+        const int from = (warp & ~(kWarps - 1)) + (lane & (kWarps - 1));
+        most = __reduce_max_sync(0xffffffffu, most_of[from]);
         if (NORM) {
-            squares = squares_of[lane & (kWarps - 1)];
+            squares = squares_of[from];
 #pragma unroll
             for (int o = kWarps / 2; o; o >>= 1) squares += __shfl_xor_sync(0xffffffffu, squares, o);
         }
@@ -366,8 +377,8 @@ struct Piece {
     float weight[VEC];
     __device__ __forceinline__ void load(const RowsParams &P, int64_t r, int c, bool whole)
     {
-        load_raw<VEC>((const T *)P.x + r * P.ldx, c, P.cols, whole, x);
-        if (NORM && P.residual) load_raw<VEC>((const T *)P.residual + r * P.ldr, c, P.cols, whole, residual);
+        load_raw<VEC, !NORM>((const T *)P.x + r * P.ldx, c, P.cols, whole, x);
+        if (NORM && P.residual) load_raw<VEC, false>((const T *)P.residual + r * P.ldr, c, P.cols, whole, residual);
     }
     // shift: how far before a multiple of VEC the row's vectors begin, the same for all threads of a row
     __device__ __forceinline__ void load_weight(const RowsParams &P, int c, bool whole, int shift)
@@ -378,11 +389,12 @@ struct Piece {
         if constexpr (VEC == 8) {
             // fp32 weights at an odd place: three aligned pieces, moved down by one and by two
             const int off = c & 3;
-            if (shift && P.weight_f32 && P.weight_whole && c >= off && c - off + 12 <= P.cols) {
+            if (shift && P.weight_f32 && P.weight_whole) {
                 float w[12];
 #pragma unroll
                 for (int i = 0; i < 3; ++i) {
-                    const float4 v = reinterpret_cast<const float4 *>((const float *)P.weight + c - off)[i];
+                    const int at = c - off + 4 * i;          // a piece that holds a weight of the row, or none
+                    const float4 v = at + 4 > 0 && at < P.cols ? *reinterpret_cast<const float4 *>((const float *)P.weight + at) : make_float4(0.f, 0.f, 0.f, 0.f);
                     w[4 * i] = v.x; w[4 * i + 1] = v.y; w[4 * i + 2] = v.z; w[4 * i + 3] = v.w;
                 }
 #pragma unroll
@@ -395,12 +407,12 @@ struct Piece {
         whole = whole && shift == 0 && P.weight_whole;
         if (P.weight_f32) {
             Raw<VEC, float> w;
-            load_raw<VEC>((const float *)P.weight, c, P.cols, whole, w);
+            load_raw<VEC, false>((const float *)P.weight, c, P.cols, whole, w);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) weight[e] = w.e[e];
         } else {
             Raw<VEC, __nv_bfloat16> w;
-            load_raw<VEC>((const __nv_bfloat16 *)P.weight, c, P.cols, whole, w);
+            load_raw<VEC, false>((const __nv_bfloat16 *)P.weight, c, P.cols, whole, w);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) weight[e] = to_float(w.e[e]);
         }
@@ -442,9 +454,9 @@ struct Piece {
 // length); the vectors are those of the memory, a row's first begins up to VEC - 1 values before it, and x, residual and total
 // have to lie alike.  The weight's values and, where q's rows lie otherwise, the 8-bit ones are then taken one by one.
 template <typename T, int VEC, bool SHIFTED, int N, int TPR, bool NORM>
-__global__ void __launch_bounds__(TPR < 64 ? 128 : TPR) rows8_kernel(const __grid_constant__ RowsParams P)
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) rows8_kernel(const __grid_constant__ RowsParams P)
 {
-    constexpr int kPer = TPR < 64 ? 128 / TPR : 1, kPieces = N / VEC;
+    constexpr int kPer = TPR < 128 ? 128 / TPR : 1, kPieces = N / VEC;
     grid_launch_dependents();
     grid_dependency_wait();
     int64_t r = (int64_t)blockIdx.x * kPer + threadIdx.x / TPR;
@@ -555,8 +567,8 @@ __global__ void __launch_bounds__(1024) rows8_long_kernel(const __grid_constant_
 template <typename T, int VEC, bool SHIFTED, int N, int TPR, bool NORM>
 cudaError_t launch_rows(const RowsParams &P, cudaStream_t st)
 {
-    constexpr int per = TPR < 64 ? 128 / TPR : 1;
-    return launch_overlapped(rows8_kernel<T, VEC, SHIFTED, N, TPR, NORM>, dim3((unsigned)(((int64_t)P.rows + per - 1) / per)), TPR < 64 ? 128u : (unsigned)TPR, 0, st, P);
+    constexpr int per = TPR < 128 ? 128 / TPR : 1;
+    return launch_overlapped(rows8_kernel<T, VEC, SHIFTED, N, TPR, NORM>, dim3((unsigned)(((int64_t)P.rows + per - 1) / per)), TPR < 128 ? 128u : (unsigned)TPR, 0, st, P);
 }
 // Values and threads for a row.  With many rows few threads with many values each: loads in flight, and what a row costs every
 // thread (sums, divisions) spread over them (8192 x 4096 bf16, norm: 128 threads 45.3 us, 256 47.3, 512 78).  With few rows, where
@@ -577,6 +589,9 @@ cudaError_t launch_rows(const RowsParams &P, bool few, cudaStream_t st)
     if (n <= 512) return launch_rows<T, 8, SHIFTED, 16, 32, NORM>(P, st);
     if (n <= 768) return launch_rows<T, 8, SHIFTED, 24, 32, NORM>(P, st);
     if (n <= 1024) return launch_rows<T, 8, SHIFTED, 32, 32, NORM>(P, st);
+    if constexpr (!NORM && !SHIFTED && sizeof(T) == 2) {       // few registers: a warp to a row goes further (16384 x 1280 13.7 -> 12.0 us)
+        if (n <= 1280) return launch_rows<T, 8, SHIFTED, 40, 32, NORM>(P, st);
+    }
     if (n <= 1536) return launch_rows<T, 8, SHIFTED, 24, 64, NORM>(P, st);
     if (n <= 2048) return launch_rows<T, 8, SHIFTED, 32, 64, NORM>(P, st);
     if (n <= 4096) return launch_rows<T, 8, SHIFTED, 32, 128, NORM>(P, st);
