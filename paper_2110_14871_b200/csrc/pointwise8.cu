@@ -157,10 +157,11 @@ gdws_status_t p8_any(const P8Params &P, cudaStream_t st)
 // slower there unless a cluster shares its sum, which costs a microsecond: 1 x 4096 -> 4096 6.8 us, here 3.9.)
 // ------------------------------------------------------------------------------------------
 constexpr int kFewD = 4, kFewRows = 8;
+// (Not through the read-only path: this kernel may have started before the one that writes w ended.)
 __device__ __forceinline__ int4 load_weights(const int8_t *p)
 {
     int4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.L2::256B.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    asm volatile("ld.global.L1::no_allocate.L2::256B.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
 
@@ -200,7 +201,7 @@ __global__ void __launch_bounds__(256) p8_few_kernel(const __grid_constant__ P8P
             for (int i = 0; i < kAhead; ++i)
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
-                    const int4 b = k + i * share * 512 < whole ? __ldg(reinterpret_cast<const int4 *>(x[r] + k + i * share * 512)) : make_int4(0, 0, 0, 0);
+                    const int4 b = k + i * share * 512 < whole ? *reinterpret_cast<const int4 *>(x[r] + k + i * share * 512) : make_int4(0, 0, 0, 0);
 #pragma unroll
                     for (int c = 0; c < kFewD; ++c) acc[c][r] = dot16(a[i][c], b, acc[c][r]);
                 }
@@ -471,7 +472,8 @@ __global__ void __launch_bounds__(256, 1) p8_slices_kernel(const __grid_constant
 
 // Many outputs: pairs of blocks (cta_group::2) compute 256 channels x 256 rows, each block's tensor memory holding its 128
 // channels; persistent, two accumulators, so that a tile's epilogue passes under the next one's products.  A pair fetches 64 KB
-// for 256 x 256 x 128 products, each block half of either operand.
+// for 256 x 256 x 128 products, each block half of either operand.  4096 x 4096 -> 4096: 51 us, 2690 Tera-operations/s (71 % of the
+// tensor pipe's cycles); 8192 x 4096 -> 8192 180 us in short runs, 216 under sustained load, where the power limit lowers the clocks.
 constexpr int kPairStages = 6;
 constexpr int kPairStage = 32768;
 constexpr int kPairSmem = 1024 + kPairStages * kPairStage;
