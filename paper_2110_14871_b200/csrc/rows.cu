@@ -159,8 +159,8 @@ union Raw {
 };
 // c may be negative.  whole: all of them exist and lie on a boundary of 16 bytes.  Others are taken one by one, or, where they are
 // known to lie on such a boundary (ALIGNED), as every piece that holds a value of the row, and what else it holds is set to zero.
-// (1000 x 10001, quantization: 21 us one by one, 13.5 by pieces.  With a residual and a weight to load it was slower by pieces, 8192
-// x 4096 46 -> 60 us, whatever the order of the conditions.)
+// (1000 x 10001, quantization: 21 us one by one, 13.5 by pieces.  Norms of rows on boundaries, whose only such vector is the last, were
+// slower by pieces: 8192 x 4096 46 -> 60 us, whatever the order of the conditions.)
 template <int VEC, bool ALIGNED, typename T>
 __device__ __forceinline__ void load_raw(const T *row, int c, int cols, bool whole, Raw<VEC, T> &b)
 {
@@ -371,14 +371,14 @@ __device__ __forceinline__ float row_scale(uint32_t most, float squares, const R
 }
 
 // VEC values of a row: x, what is added to it and what multiplies it, and from them h and u.
-template <typename T, int VEC, bool NORM>
+template <typename T, int VEC, bool SHIFTED, bool NORM>
 struct Piece {
     Raw<VEC, T> x, residual;
     float weight[VEC];
     __device__ __forceinline__ void load(const RowsParams &P, int64_t r, int c, bool whole)
     {
-        load_raw<VEC, !NORM>((const T *)P.x + r * P.ldx, c, P.cols, whole, x);
-        if (NORM && P.residual) load_raw<VEC, false>((const T *)P.residual + r * P.ldr, c, P.cols, whole, residual);
+        load_raw<VEC, !NORM || SHIFTED>((const T *)P.x + r * P.ldx, c, P.cols, whole, x);
+        if (NORM && P.residual) load_raw<VEC, SHIFTED>((const T *)P.residual + r * P.ldr, c, P.cols, whole, residual);
     }
     // shift: how far before a multiple of VEC the row's vectors begin, the same for all threads of a row
     __device__ __forceinline__ void load_weight(const RowsParams &P, int c, bool whole, int shift)
@@ -473,7 +473,7 @@ __global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) rows8_kernel(const __gr
     // bf16 values that nothing is added to stay as they are, two to a register: half of the registers, more rows at a time
     constexpr bool kPacked = !NORM && VEC == 8 && sizeof(T) == 2;
     float u[kPacked ? 1 : N], most = 0.f, squares[2] = {};
-    Piece<T, VEC, NORM> p[kPieces];
+    Piece<T, VEC, SHIFTED, NORM> p[kPieces];
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) p[i].load(P, r, column(i), whole(column(i)));
     if constexpr (kPacked) {
@@ -541,7 +541,7 @@ __global__ void __launch_bounds__(1024) rows8_long_kernel(const __grid_constant_
     const int64_t r = blockIdx.x;
     float most = 0.f, squares[2] = {};
     for (int c = threadIdx.x; c < P.cols; c += 1024) {
-        Piece<T, 1, NORM> p;
+        Piece<T, 1, false, NORM> p;
         float u[1];
         p.load(P, r, c, false);
         p.load_weight(P, c, false, 0);
@@ -554,7 +554,7 @@ __global__ void __launch_bounds__(1024) rows8_long_kernel(const __grid_constant_
     float m = fine ? __uint_as_float(top) : 0.f;
     const float lift = lifted(m), inv = m > 0.f ? 127.f / m : 0.f;
     for (int c = threadIdx.x; c < P.cols; c += 1024) {
-        Piece<T, 1, NORM> p;
+        Piece<T, 1, false, NORM> p;
         float u[1];
         int q[1];
         p.load(P, r, c, false);
@@ -589,6 +589,11 @@ cudaError_t launch_rows(const RowsParams &P, bool few, cudaStream_t st)
     if (n <= 128) return launch_rows<T, 8, SHIFTED, 16, 8, NORM>(P, st);
     if (n <= 256) return launch_rows<T, 8, SHIFTED, 16, 16, NORM>(P, st);
     if (n <= 512) return launch_rows<T, 8, SHIFTED, 16, 32, NORM>(P, st);
+    if constexpr (NORM && SHIFTED) {       // more registers a value: fewer values where that is not half of the threads more (10000 x 801 bf16 31.8 -> 24.5 us)
+        if (n > 768 && n <= 1024) return launch_rows<T, 8, SHIFTED, 16, 64, NORM>(P, st);
+        if (n > 1536 && n <= 2048) return launch_rows<T, 8, SHIFTED, 16, 128, NORM>(P, st);
+        if (n > 2048 && n <= 4096) return launch_rows<T, 8, SHIFTED, 16, 256, NORM>(P, st);
+    }
     if (n <= 768) return launch_rows<T, 8, SHIFTED, 24, 32, NORM>(P, st);
     if (n <= 1024) return launch_rows<T, 8, SHIFTED, 32, 32, NORM>(P, st);
     if constexpr (!NORM && !SHIFTED && sizeof(T) == 2) {       // few registers: a warp to a row goes further (16384 x 1280 13.7 -> 12.0 us)
@@ -597,9 +602,16 @@ cudaError_t launch_rows(const RowsParams &P, bool few, cudaStream_t st)
     if (n <= 1536) return launch_rows<T, 8, SHIFTED, 24, 64, NORM>(P, st);
     if (n <= 2048) return launch_rows<T, 8, SHIFTED, 32, 64, NORM>(P, st);
     if (n <= 4096) return launch_rows<T, 8, SHIFTED, 32, 128, NORM>(P, st);
+    if constexpr (NORM && (SHIFTED || sizeof(T) == 4)) {       // more registers a value: fewer values (4000 x 7999 bf16 79 -> 69 us, 2000 x 7000 fp32 42 -> 36)
+        if (SHIFTED && n <= 6144) return launch_rows<T, 8, SHIFTED, 24, 256, NORM>(P, st);
+        if (n <= 8192) return launch_rows<T, 8, SHIFTED, 16, 512, NORM>(P, st);
+    }
     if (n <= 6144) return launch_rows<T, 8, SHIFTED, 24, 256, NORM>(P, st);
     if (n <= 8192) return launch_rows<T, 8, SHIFTED, 32, 256, NORM>(P, st);
     if (n <= 12288) return launch_rows<T, 8, SHIFTED, 24, 512, NORM>(P, st);
+    if constexpr (NORM) {        // 32 values and what is added to them leave one block of 512 threads on an SM (2000 x 16000 bf16 64 -> 56 us)
+        if (n <= 16384) return launch_rows<T, 8, SHIFTED, 16, 1024, NORM>(P, st);
+    }
     if (n <= 16384) return launch_rows<T, 8, SHIFTED, 32, 512, NORM>(P, st);
     if (n <= 32768) return launch_rows<T, 8, SHIFTED, 32, 1024, NORM>(P, st);
     return launch_overlapped(rows8_long_kernel<T, NORM>, dim3((unsigned)P.rows), 1024u, 0, st, P);

@@ -60,6 +60,18 @@ def test_sizes(rows, K, D, out, relu, bias):
     compare(rows, K, D, out, bias, relu, seed=rows + K + D)
 
 
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,K,D,kernel", [(4100, 300, 2301, gdws.KERNEL8_PAIRS), (2561, 1000, 2600, gdws.KERNEL8_PAIRS), (9000, 100, 1030, gdws.KERNEL8_PAIRS), (300, 5000, 5001, gdws.KERNEL8_SLICES),
+                                             (20, 131071, 300, gdws.KERNEL8_SLICES), (40, 3000, 2000, gdws.KERNEL8_SLICES), (100, 8000, 500, gdws.KERNEL8_SLICES), (500, 640, 700, gdws.KERNEL8_SLICES),
+                                             (6, 5000, 130, gdws.KERNEL8_FEW), (3, 70000, 9, gdws.KERNEL8_FEW), (1, 200, 20001, gdws.KERNEL8_SLICES)])
+def test_every_kernel(rows, K, D, kernel, out):
+    """Several tiles for each pair of SMs, rings that go round, clusters of every size, warps that share columns."""
+    y = compare(rows, K, D, out, True, True, seed=rows)
+    x, xs = rows8(rows, K, 1, ceil16(K))
+    w, ws = rows8(D, K, 2, ceil16(K))
+    assert kernel == gdws.pointwise8_kernel(x.t, xs, w.t, ws, y)
+
+
 @pytest.mark.parametrize("rows,K,D,ldx,ldw,shift", [(5, 1337, 70, 1337, 1337, 0), (70, 100, 130, 100, 112, 0), (70, 100, 130, 112, 101, 0), (40, 96, 50, 96, 96, 4), (3, 64, 64, 64, 64, 1), (150, 515, 90, 516, 516, 0)])
 def test_any_alignment(rows, K, D, ldx, ldw, shift):
     compare(rows, K, D, "f32", True, False, ldx, ldw, shift)

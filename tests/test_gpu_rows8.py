@@ -90,6 +90,31 @@ def test_norm_quantize(rows, cols, gap, shift, dtype, residual, total, weight):
             f.check("a matrix")
 
 
+@pytest.mark.parametrize("odd", [0, 1])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cols", [16, 32, 56, 120, 240, 440, 700, 960, 1240, 1496, 1960, 2960, 4064, 6000, 8000, 12000, 16000])
+def test_more_rows_than_fill_the_chip(cols, dtype, odd):
+    """As many rows as take the threads per row that large calls do; the last block has a row too few."""
+    cols += odd
+    rows = 2_600_000 // cols + 3
+    x, r = values(rows, cols, dtype, cols), values(rows, cols, dtype, cols + 1)
+    w = 1 + 0.2 * values(1, cols, "f32", 3)[0]
+    q, scale = Field(rows, cols, torch.int8, (cols + 15) // 16 * 16), Field(1, rows, torch.float32)
+    total, y = Field(rows, cols, TYPES[dtype]), Field(rows, cols, TYPES[dtype])
+    gdws.quantize_rows(x, q.t, scale.t[0])
+    want, want_scale = steps_of(x.float())
+    assert torch.equal(q.t, want) and torch.equal(scale.t[0], want_scale)
+    gdws.norm_quantize_rows(x, q.t, scale.t[0], weight=w, residual=r, total=total.t)
+    h = x.float() + r.float()
+    assert torch.equal(q.t, steps_of(h * w)[0]) and torch.equal(total.t, h.to(TYPES[dtype]))
+    want_scale = (h * w).double().abs().amax(1) / 127 / torch.sqrt(h.double().square().mean(1) + 1e-6)
+    assert ((scale.t[0].double() - want_scale).abs() <= norm_bound(cols) * want_scale).all()
+    gdws.dequantize_rows(q.t, scale.t[0], y.t)
+    assert torch.equal(y.t, (q.t.float() * scale.t[0][:, None]).to(TYPES[dtype]))
+    for f in (q, scale, total, y):
+        f.check("a matrix")
+
+
 @pytest.mark.parametrize("cols", [5, 61, 130, 1000, 1333, 5003, 20001])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_matrices_that_lie_differently(dtype, cols):
