@@ -401,6 +401,12 @@ struct Piece {
                 for (int e = 0; e < 11; ++e) w[e] = off & 1 ? w[e + 1] : w[e];
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) weight[e] = off & 2 ? w[e + 2] : w[e];
+                // what the last piece holds behind the weight is not the caller's: zero times it may be NaN
+                if (!whole) {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e)
+                        if ((unsigned)(c + e) >= (unsigned)P.cols) weight[e] = 0.f;
+                }
                 return;
             }
         }
