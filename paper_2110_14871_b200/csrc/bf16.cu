@@ -121,8 +121,10 @@ __global__ void __launch_bounds__(kPwThreads, 1) pw_bf16_tc_kernel(const __grid_
         fence_mbar_init();
     }
     __syncwarp();
-    grid_launch_dependents();
-    if (warp == 1) tmem_alloc(smem_u32(&tmem_slot), (uint32_t)(P.nacc * P.acc_cols));
+    if (warp == 1) {
+        tmem_alloc(smem_u32(&tmem_slot), (uint32_t)(P.nacc * P.acc_cols));
+        grid_launch_dependents();
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();

@@ -310,8 +310,10 @@ __global__ void __launch_bounds__(kF32TcThreads, 1) f32_tc_kernel(const __grid_c
         mbar_init(bar_drain, 1);
         fence_mbar_init();
     }
-    grid_launch_dependents();
-    if (warp == kF32TcMmaWarp) tmem_alloc(smem_u32(&tmem_slot), 64u * NB);
+    if (warp == kF32TcMmaWarp) {
+        tmem_alloc(smem_u32(&tmem_slot), 64u * NB);
+        grid_launch_dependents();
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();

@@ -201,7 +201,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFoldThreads, 1) fol
         mbar_init(bar_afull + 8 * (uint32_t)tid, acc >= kFoldMaxAcc && acc < 2 * kFoldMaxAcc ? 8u * (uint32_t)P.gb : (tid == kBars - 2 ? 2u : 1u));
         fence_mbar_init();
     }
-    grid_launch_dependents();
     if (warp == kFoldAWarp && lane == 0) {
 #pragma unroll 1
         for (int l = 0; l < 4; ++l)
@@ -211,7 +210,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kFoldThreads, 1) fol
     } else if (warp == kFoldEpiWarp0 && lane == 0) {
         prefetch_tensor_map(&P.tmap_y);
     }
-    if (warp == kFoldTmemWarp) tmem_alloc_pair(smem_u32(&tmem_slot), (uint32_t)(P.nacc * P.acc_cols));
+    if (warp == kFoldTmemWarp) {
+        tmem_alloc_pair(smem_u32(&tmem_slot), (uint32_t)(P.nacc * P.acc_cols));
+        grid_launch_dependents();
+    }
     tc_fence_before();
     __syncthreads();
     cluster_sync();              // both blocks' barriers are initialised before either signals the other's

@@ -65,10 +65,12 @@ __global__ void __launch_bounds__(kSplitThreads, 1) fold_split_kernel(const __gr
         mbar_init(bar_full + 8 * (uint32_t)tid, 1);
         fence_mbar_init();
     }
-    grid_launch_dependents();
     if (warp == kSplitAWarp && lane < 4 && ((P.maps_used >> lane) & 1)) prefetch_tensor_map(&P.tmap_x[lane]);
     if (warp == kSplitBWarp && lane == 0) prefetch_tensor_map(&P.tmap_w);
-    if (warp == kSplitTermWarp) tmem_alloc(smem_u32(&tmem_slot), (uint32_t)P.acc_cols);
+    if (warp == kSplitTermWarp) {
+        tmem_alloc(smem_u32(&tmem_slot), (uint32_t)P.acc_cols);
+        grid_launch_dependents();
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();

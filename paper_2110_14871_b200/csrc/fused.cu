@@ -442,7 +442,6 @@ __global__ void __launch_bounds__(kFusedThreads, 1) fused_bf16_kernel(const __gr
     const uint32_t w_s = x_s + (uint32_t)P.nslots * P.slot_bytes;         // ring of nwslots filter blocks
     int4 *meta_tab = reinterpret_cast<int4 *>(base + (w_s - a_s) + (size_t)P.nwslots * wblock);
 
-    grid_launch_dependents();      // the next kernel in the stream may start its prologue as SMs become free
     if (tid == 0) abort_flag = 0;
     {
         // Eight threads of warp 1 initialise the barriers, one ring slot each (warp 0 allocates tensor memory meanwhile).
@@ -466,7 +465,10 @@ __global__ void __launch_bounds__(kFusedThreads, 1) fused_bf16_kernel(const __gr
             fence_mbar_init();
         }
     }
-    if (!ZOUT && warp == kCtrlWarp) tmem_alloc(smem_u32(&tmem_slot), (uint32_t)(P.nacc * P.acc_cols));
+    if (warp == kCtrlWarp) {
+        if (!ZOUT) tmem_alloc(smem_u32(&tmem_slot), (uint32_t)(P.nacc * P.acc_cols));
+        grid_launch_dependents();      // the next kernel in the stream may start its prologue as SMs become free
+    }
     // up to here only this block's shared and tensor memory were touched; the kernel before this one in the stream has
     // to be complete before global memory is read or written
     grid_dependency_wait();

@@ -175,10 +175,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) fused_tc_kernel(const __grid_co
             fence_mbar_init();
         }
     }
-    // The kernel that follows in the stream (launched with programmatic serialisation, as this one is) may start its
+    // Then the kernel that follows in the stream (launched with programmatic serialisation, as this one is) may start its
     // blocks as SMs become free; it reads nothing from global memory before its own grid_dependency_wait below.
-    grid_launch_dependents();
-    if (warp == 0) tmem_alloc(smem_u32(&tmem_slot), 512u);
+    if (warp == 0) {
+        tmem_alloc(smem_u32(&tmem_slot), 512u);
+        grid_launch_dependents();
+    }
     {
         for (int i = tid; i < P.nb * 128; i += kTcThreads) bold[i] = 0xFFFFu;
         const uint4 zero = make_uint4(0u, 0u, 0u, 0u);

@@ -159,13 +159,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGdwThreads, 1) gdw_
         mbar_init(bar_afull + 8 * (uint32_t)tid, many ? 8u : 1u);
         fence_mbar_init();
     }
-    grid_launch_dependents();
     if (warp == kGdwAWarp && lane == 0) {
 #pragma unroll 1
         for (int l = 0; l < 4; ++l)
             if ((P.maps_used >> l) & 1) prefetch_tensor_map(&P.tmap_x[l]);
     }
-    if (warp == kGdwTmemWarp) tmem_alloc_pair(smem_u32(&tmem_slot), 64u * kGdwAcc);
+    if (warp == kGdwTmemWarp) {
+        tmem_alloc_pair(smem_u32(&tmem_slot), 64u * kGdwAcc);
+        grid_launch_dependents();
+    }
     for (int q = tid; q < P.nchunks; q += kGdwThreads) {         // written when the plan was made
         if (P.resident) {
             chunks[q] = (int)P.info[q];

@@ -158,7 +158,8 @@ void plan_count(int device, int change);       // plans that hold memory of the 
 
 // Launch with programmatic stream serialisation: the kernel may be scheduled while the kernel before it in the stream
 // is still running (once all blocks of that one have executed griddepcontrol.launch_dependents, which the library's
-// kernels do first thing).  Such a kernel touches global memory only after its own griddepcontrol.wait.
+// kernels do first thing, or as soon as they have their tensor memory).  Such a kernel touches global memory only after its own
+// griddepcontrol.wait.
 template <class... KArgs, class... Args>
 inline cudaError_t launch_overlapped(void (*kernel)(KArgs...), dim3 grid, unsigned block, size_t smem, cudaStream_t st, Args &&...args)
 {

@@ -392,9 +392,11 @@ __global__ void __launch_bounds__(256, 1) p8_slices_kernel(const __grid_constant
         fence_mbar_init();
     }
     __syncwarp();
-    grid_launch_dependents();
     if (warp == 0 && lane == 0) { prefetch_tensor_map(&P.tw); prefetch_tensor_map(&P.tx); }
-    if (warp == 2) tmem_alloc(smem_u32(&tmem_slot), cols);
+    if (warp == 2) {
+        tmem_alloc(smem_u32(&tmem_slot), cols);
+        grid_launch_dependents();
+    }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -509,9 +511,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1) p8_
         fence_mbar_init();
     }
     __syncwarp();
-    grid_launch_dependents();
     if (warp == 0 && lane == 0) { prefetch_tensor_map(&P.tw); prefetch_tensor_map(&P.tx); }
-    if (warp == 2) tmem_alloc_pair(smem_u32(&tmem_slot), 512);
+    if (warp == 2) {
+        tmem_alloc_pair(smem_u32(&tmem_slot), 512);
+        grid_launch_dependents();
+    }
     tc_fence_before();
     __syncthreads();
     cluster_sync();              // both blocks' barriers are initialised before either signals the other's
@@ -785,7 +789,8 @@ gdws_status_t p8_tc(const P8Params &A, const P8Choice &c, int device, int sms, c
         P.per_shift = 0;
         while (c.split << P.per_shift < c.nt) ++P.per_shift;
         // Blocks of a cluster that wait for each other hold tensor memory meanwhile.  Two such kernels on one SM could each hold what
-        // a block of the other's clusters waits for, so they take more than half of the shared memory: one block per SM.
+        // a block of the other's clusters waits for, so they take more than half of the shared memory: one block per SM.  (Blocks that
+        // wait for nobody may share an SM with any kernel: see grid_launch_dependents on what the order of allocations has to be.)
         const size_t need = 1024 + (size_t)P.recv + recv;
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)blocks); cfg.blockDim = dim3(256); cfg.stream = st;

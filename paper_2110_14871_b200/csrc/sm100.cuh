@@ -59,6 +59,10 @@ __device__ __forceinline__ uint32_t mbar_try_wait(uint32_t bar, uint32_t parity)
 // grid_dependency_wait: returns once the kernel before this one in the stream has completed and its writes are visible
 // (at once when this kernel was not launched with the attribute).  A kernel must execute it, in every thread that
 // touches global memory afterwards, before its first global access.
+// A kernel with tensor memory launches its dependents behind its allocation, in the warp that allocates (the first invocation in
+// a block is the block's).  Its dependents allocate before they wait for it, on the same SMs, and an allocation that finds no
+// columns waits without a limit: dependents that started first could hold what this kernel's blocks still need, while they
+// wait for this kernel to end.  So a block that waits for the kernel before it waits for one that has all its columns.
 __device__ __forceinline__ void grid_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 // Bounded wait.  When the limit runs out (about a second) the thread records `code` in the
