@@ -2,7 +2,8 @@
 // is that of the host: through the ctypes binding 3.6 us of a product's 6.4 went into asking tensors for their shape and address.
 //
 // Each function returns the call's status, or -1 where an argument is anything but an ordinary tensor that the call takes as it is;
-// gdws.py then goes through the same checks one by one and says what is wrong, or takes the call itself.
+// gdws.py then goes through the same checks one by one and says what is wrong, or takes the call itself.  So it does where torch
+// throws: the tensors of a functional transform (vmap, grad) have the ordinary type but no memory of their own.
 #include <Python.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -20,7 +21,7 @@ const at::Tensor *tensor(PyObject *o, long device)
 {
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor &t = THPVariable_Unpack(o);
-    return t.is_cuda() && t.get_device() == device && t.layout() == at::kStrided && !t.is_conj() && !t.is_neg() ? &t : nullptr;
+    return t.has_storage() && t.is_cuda() && t.get_device() == device && t.layout() == at::kStrided && !t.is_conj() && !t.is_neg() ? &t : nullptr;
 }
 
 bool geometry(const at::Tensor &t, int64_t *rows, int64_t *ld, int *cols)
@@ -76,13 +77,18 @@ bool place(long *device, void **stream)
     return !PyErr_Occurred();
 }
 
+struct WithoutGil {
+    PyThreadState *state = PyEval_SaveThread();
+    ~WithoutGil() { PyEval_RestoreThread(state); }
+};
 template <class Call>
 PyObject *status_of(Call call)
 {
     gdws_status_t st;
-    Py_BEGIN_ALLOW_THREADS
-    st = call();
-    Py_END_ALLOW_THREADS
+    {
+        WithoutGil released;
+        st = call();
+    }
     return PyLong_FromLong((long)st);
 }
 PyObject *other() { return PyLong_FromLong(-1); }
@@ -168,12 +174,26 @@ PyObject *pointwise8(PyObject *, PyObject *const *a, Py_ssize_t n)              
     return status_of([&] { return g_product(&x, &w, bias, relu, &y, stream); });
 }
 
+// Nothing is thrown into the interpreter, which is C.
+template <PyObject *(*function)(PyObject *, PyObject *const *, Py_ssize_t)>
+PyObject *guarded(PyObject *self, PyObject *const *a, Py_ssize_t n)
+{
+    try {
+        return function(self, a, n);
+    } catch (...) {
+        PyErr_Clear();
+        return other();
+    }
+}
+template <PyObject *(*function)(PyObject *, PyObject *const *, Py_ssize_t)>
+PyCFunction method() { return (PyCFunction)(void (*)(void))guarded<function>; }
+
 PyMethodDef g_methods[] = {
     {"bind", (PyCFunction)(void (*)(void))bind, METH_FASTCALL, nullptr},
-    {"quantize_rows", (PyCFunction)(void (*)(void))quantize_rows, METH_FASTCALL, nullptr},
-    {"dequantize_rows", (PyCFunction)(void (*)(void))dequantize_rows, METH_FASTCALL, nullptr},
-    {"norm_quantize_rows", (PyCFunction)(void (*)(void))norm_quantize_rows, METH_FASTCALL, nullptr},
-    {"pointwise8", (PyCFunction)(void (*)(void))pointwise8, METH_FASTCALL, nullptr},
+    {"quantize_rows", method<quantize_rows>(), METH_FASTCALL, nullptr},
+    {"dequantize_rows", method<dequantize_rows>(), METH_FASTCALL, nullptr},
+    {"norm_quantize_rows", method<norm_quantize_rows>(), METH_FASTCALL, nullptr},
+    {"pointwise8", method<pointwise8>(), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_rows", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
