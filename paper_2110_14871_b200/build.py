@@ -1,7 +1,9 @@
 """Build libgdws.so in-tree with nvcc for sm_100a (cross-compiles without a GPU)."""
 from __future__ import annotations
 
+import importlib.metadata
 import os
+import shutil
 import subprocess
 import sys
 
@@ -13,6 +15,7 @@ HEADERS = [os.path.join(CSRC, "gdws_internal.h"), os.path.join(CSRC, "sm100.cuh"
 LIB_PATH = os.path.join(_HERE, "libgdws.so")
 BINDING = os.path.join(CSRC, "rows_binding.cpp")      # the calls on rows for Python, against torch's headers
 BINDING_PATH = os.path.join(_HERE, "_rows.so")
+BINDING_FOR = os.path.join(_HERE, "_build", "rows_binding.txt")      # the versions that it was built against
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
@@ -27,10 +30,29 @@ def _nvcc() -> str:
     return "nvcc"
 
 
-def build_binding(force: bool = False) -> str:
-    """Compile ``_rows.so`` (host code only) next to this file; returns its path."""
+def _torch_version():
+    """The version of torch that the binding would be built against; None where there is no torch."""
+    try:
+        return importlib.metadata.version("torch")
+    except importlib.metadata.PackageNotFoundError:
+        return None
+
+
+def binding_is_stale() -> bool:
+    """Whether ``_rows.so`` is missing, older than its sources, or built against another torch or Python, whose C++ interfaces it uses."""
     deps = [BINDING, os.path.join(_ROOT, "include", "gdws.h")]
-    if not force and os.path.exists(BINDING_PATH) and all(os.path.getmtime(d) <= os.path.getmtime(BINDING_PATH) for d in deps):
+    if not os.path.exists(BINDING_PATH) or any(os.path.getmtime(d) > os.path.getmtime(BINDING_PATH) for d in deps):
+        return True
+    try:
+        with open(BINDING_FOR) as f:
+            return f.read() != f"{_torch_version()} {sys.version}"
+    except OSError:
+        return True
+
+
+def build_binding(force: bool = False) -> str:
+    """Compile ``_rows.so`` (host code only, against torch's headers, by g++) next to this file; returns its path."""
+    if not force and not binding_is_stale():
         return BINDING_PATH
     import sysconfig
     import torch
@@ -40,6 +62,9 @@ def build_binding(force: bool = False) -> str:
                            "-I", os.path.join(_ROOT, "include"), "-isystem", os.path.join(home, "include"), "-isystem", os.path.join(home, "include", "torch", "csrc", "api", "include"),
                            "-isystem", sysconfig.get_paths()["include"], BINDING, "-o", tmp, "-L" + os.path.join(home, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"])
     os.replace(tmp, BINDING_PATH)
+    os.makedirs(os.path.dirname(BINDING_FOR), exist_ok=True)
+    with open(BINDING_FOR, "w") as f:
+        f.write(f"{_torch_version()} {sys.version}")
     return BINDING_PATH
 
 
@@ -52,10 +77,16 @@ def is_stale() -> bool:
 
 
 def build_library(force: bool = False, verbose: bool = False) -> str:
-    """Compile the CUDA sources into ``libgdws.so`` and the binding of the calls on rows next to this file; returns the library's path."""
-    build_binding(force)
-    if not force and not is_stale():
-        return LIB_PATH
+    """Compile the CUDA sources into ``libgdws.so`` next to this file, and the binding of the calls on rows where there are torch and
+    g++ (the library needs neither); returns the library's path."""
+    if force or is_stale():
+        _build_cuda(verbose)
+    if _torch_version() and shutil.which("g++"):
+        build_binding(force)
+    return LIB_PATH
+
+
+def _build_cuda(verbose: bool) -> None:
     objdir = os.path.join(_HERE, "_build")
     os.makedirs(objdir, exist_ok=True)
     nvcc = _nvcc()
@@ -79,7 +110,6 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     cmd = [nvcc, "-shared", "-gencode", "arch=compute_100a,code=sm_100a", "-o", tmp, *objs]
     subprocess.check_call(cmd)
     os.replace(tmp, LIB_PATH)
-    return LIB_PATH
 
 
 if __name__ == "__main__":

@@ -6,6 +6,7 @@
 // throws: the tensors of a functional transform (vmap, grad) have the ordinary type but no memory of their own.
 #include <Python.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/version.h>
 
 #include "gdws.h"
 
@@ -200,4 +201,9 @@ PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_rows", nullptr, -1, g_methods, 
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__rows(void) { return PyModule_Create(&g_module); }
+PyMODINIT_FUNC PyInit__rows(void)
+{
+    PyObject *m = PyModule_Create(&g_module);
+    if (m && PyModule_AddStringConstant(m, "torch_version", TORCH_VERSION) < 0) Py_CLEAR(m);
+    return m;
+}

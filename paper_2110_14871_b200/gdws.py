@@ -398,6 +398,8 @@ def _rows_setup():
     if not os.path.exists(os.path.join(_HERE, "_rows.so")):
         raise FileNotFoundError("_rows.so is missing: build it with `python -m paper_2110_14871_b200.build`")
     from . import _rows as native
+    if native.torch_version != torch.__version__.split("+")[0]:
+        raise ImportError(f"_rows.so was built against torch {native.torch_version}, this is {torch.__version__}: build it anew with `python -m paper_2110_14871_b200.build`")
     if not torch.cuda.is_available():
         _get_device = lambda: -1  # noqa: E731
     else:
