@@ -321,7 +321,8 @@ GDWS_API size_t gdws_static_scratch_bytes(void);
  * threads at once are independent.  Buffers are those of the current device.
  *
  * Element (r, c) of gdws_rows_t is ptr[r * ld + c], of gdws_rows8_t it stands for scale[r] * q[r * ld + c].  rows >= 0 (at most
- * 2^31 - 1024; with 0 rows nothing is done and pointers may be NULL), 1 <= cols <= 2^30, ld >= cols (not looked at for a single row).
+ * 2^31 - 1024; with 0 rows nothing is done and pointers may be NULL), 1 <= cols <= 2^30, ld >= cols (not looked at for a single row),
+ * (rows - 1) * ld <= 2^56.
  * Pointers need the alignment of their element type only, whatever the general rule says.  Nothing but the elements themselves is
  * written, and used: neither what lies between cols and ld nor rows behind the last one (an aligned 16-byte piece that holds an
  * element may be read as a whole).  Outputs must not overlap inputs or each

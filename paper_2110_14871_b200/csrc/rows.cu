@@ -47,6 +47,8 @@ gdws_status_t check_shape(const char *call, const char *name, int64_t rows, int6
     if (rows < 0 || rows > kMostRows) return fail(GDWS_ERR_INVALID_ARG, "%s: %s->rows=%lld is outside 0..2^31-1024", call, name, (long long)rows);
     if (cols < 1 || cols > kMostCols) return fail(GDWS_ERR_INVALID_ARG, "%s: %s->cols=%lld is outside 1..2^30", call, name, (long long)cols);
     if (rows > 1 && (ld < cols || ld > ((int64_t)1 << 40) / 4)) return fail(GDWS_ERR_INVALID_ARG, "%s: %s->ld=%lld does not fit rows of %lld", call, name, (long long)ld, (long long)cols);
+    // so that the bytes of a matrix fit 64 bits, whatever its type: overlaps are looked for by address
+    if (rows > 1 && rows - 1 > ((int64_t)1 << 56) / ld) return fail(GDWS_ERR_INVALID_ARG, "%s: %s spans more than 2^56 elements", call, name);
     return GDWS_OK;
 }
 
