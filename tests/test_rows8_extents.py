@@ -21,10 +21,11 @@ def kernel_of(x, w, y):
 
 
 def test_overlaps_of_matrices_that_pass_64_bits():
-    """y lies in the middle of x in both calls; in the second x's last byte lies 2^69 behind its first."""
-    w, y = gdws.Rows8(BASE * 8, BASE * 9, 8, 64, 64), gdws.Rows(BASE + (1 << 20), MOST, 8, 8, gdws.BF16)
-    assert kernel_of(gdws.Rows8(BASE, BASE * 64, MOST, 64, 64), w, y) == gdws.ERR_INVALID_ARG and "overlap" in gdws.last_error()
-    assert kernel_of(gdws.Rows8(BASE, BASE * 64, MOST, 1 << 38, 64), w, y) == gdws.ERR_INVALID_ARG and "2^56" in gdws.last_error()
+    """y lies in x in every call.  With 2^30 + 1 rows 2^34 bytes apart the distance of x's last row from its first is 2^64: zero, in 64 bits."""
+    w = gdws.Rows8(BASE * 8, BASE * 9, 8, 64, 64)
+    for rows, ld, message in (((1 << 30) + 1, 64, "overlap"), ((1 << 30) + 1, 1 << 34, "2^56"), (MOST, 1 << 38, "2^56")):
+        y = gdws.Rows(BASE + (1 << 20), rows, 8, 8, gdws.BF16)
+        assert kernel_of(gdws.Rows8(BASE, BASE * 64, rows, ld, 64), w, y) == gdws.ERR_INVALID_ARG and message in gdws.last_error(), gdws.last_error()
 
 
 @pytest.mark.parametrize("rows,ld,fine", [(1 << 20, 1 << 36, True), ((1 << 20) + 1, 1 << 36, True), ((1 << 20) + 2, 1 << 36, False), (MOST, 1 << 25, True), (MOST, 1 << 26, False), (MOST, 1 << 38, False), (2, 1 << 38, True), (1, 1 << 62, True)])
