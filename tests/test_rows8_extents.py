@@ -22,7 +22,7 @@ def kernel_of(x, w, y):
 
 def test_overlaps_of_matrices_that_pass_64_bits():
     """y lies in x in every call.  With 2^30 + 1 rows 2^34 bytes apart the distance of x's last row from its first is 2^64: zero, in 64 bits."""
-    w = gdws.Rows8(BASE * 8, BASE * 9, 8, 64, 64)
+    w = gdws.Rows8(BASE - (1 << 20), BASE - (1 << 22), 8, 64, 64)
     for rows, ld, message in (((1 << 30) + 1, 64, "overlap"), ((1 << 30) + 1, 1 << 34, "2^56"), (MOST, 1 << 38, "2^56")):
         y = gdws.Rows(BASE + (1 << 20), rows, 8, 8, gdws.BF16)
         assert kernel_of(gdws.Rows8(BASE, BASE * 64, rows, ld, 64), w, y) == gdws.ERR_INVALID_ARG and message in gdws.last_error(), gdws.last_error()
