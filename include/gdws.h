@@ -359,7 +359,7 @@ GDWS_API gdws_status_t gdws_quantize_rows(const gdws_rows_t *x, const gdws_rows8
  *   residual   NULL: none;  total   NULL: not written.  Type, rows and cols of x.  total may be the very rows of x or of residual
  *   weight     DEVICE, cols entries of weight_dtype (F32 or BF16), NULL: ones
  *   eps        finite, at least 2^-126
- * Sums are fp32.  A row with an infinity or NaN in x, residual, h * weight or the sum of squares gets scale NaN and zeros.
+ * Sums are fp32, those of long rows partly in 64 bits.  A row with an infinity or NaN in x, residual, h * weight or the sum of squares gets scale NaN and zeros.
  * Errors: as gdws_quantize_rows.
  */
 GDWS_API gdws_status_t gdws_norm_quantize_rows(const gdws_rows_t *x, const gdws_rows_t *residual, const gdws_rows_t *total,
