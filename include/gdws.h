@@ -439,6 +439,9 @@ GDWS_API gdws_status_t gdws_measure_code_size(int body_instructions, int threads
  */
 GDWS_API gdws_status_t gdws_selftest_wait(gdws_plan_t *plan, unsigned int polls, void *stream);
 
+/* gdws_rows_selftest_wait -- the same for the status word of the calls on rows, which gdws_rows_status reports. */
+GDWS_API gdws_status_t gdws_rows_selftest_wait(unsigned int polls, void *stream);
+
 /* Number of kernels this plan has launched so far (all entry points). */
 GDWS_API int64_t gdws_launch_count(const gdws_plan_t *plan);
 

@@ -1,6 +1,6 @@
 // Diagnostics of libgdws: a measurement of the multiply-add rate of the plain ALUs (the bound of a GDW stage
 // that runs there) and a self-test of the bounded-wait error path.
-#include "sm100.cuh"
+#include "rows.cuh"
 
 using namespace gdws;
 
@@ -224,6 +224,18 @@ gdws_status_t gdws_selftest_wait(gdws_plan_t *p, unsigned int polls, void *strea
     p->launches++;
     cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? GDWS_OK : cuda_fail(e, "wait_selftest_kernel launch");
+}
+
+gdws_status_t gdws_rows_selftest_wait(unsigned int polls, void *stream)
+{
+    if (polls > (1u << 16)) return fail(GDWS_ERR_INVALID_ARG, "gdws_rows_selftest_wait: at most 65536 polls");
+    int device, sms, *word = nullptr;
+    const gdws_status_t st = rows_device(&device, &sms);
+    if (st != GDWS_OK) return st;
+    const cudaError_t e = rows_status_word(&word);
+    if (e != cudaSuccess) return cuda_fail(e, "status word of the calls on rows");
+    wait_selftest_kernel<<<1, 64, 0, (cudaStream_t)stream>>>(word, polls);
+    return launched(cudaGetLastError(), "wait_selftest_kernel launch");
 }
 
 }  // extern "C"

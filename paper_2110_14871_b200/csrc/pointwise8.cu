@@ -817,6 +817,9 @@ P8Params p8_params(const gdws_rows8_t *x, const gdws_rows8_t *w, const float *bi
 }
 
 }  // namespace
+
+cudaError_t rows_status_word(int **word) { return cudaGetSymbolAddress((void **)word, g_rows_status); }
+
 }  // namespace gdws
 
 using namespace gdws;
@@ -860,10 +863,9 @@ gdws_status_t gdws_rows_status(void)
     int device, sms;
     const gdws_status_t st = rows_device(&device, &sms);
     if (st != GDWS_OK) return st;
-    int word = 0;
-    void *at = nullptr;
+    int word = 0, *at = nullptr;
     cudaError_t e = cudaDeviceSynchronize();
-    if (e == cudaSuccess) e = cudaGetSymbolAddress(&at, g_rows_status);
+    if (e == cudaSuccess) e = rows_status_word(&at);
     if (e == cudaSuccess) e = cudaMemcpy(&word, at, sizeof(int), cudaMemcpyDeviceToHost);
     if (e == cudaSuccess && word) e = cudaMemset(at, 0, sizeof(int));
     if (e != cudaSuccess) return cuda_fail(e, "status read");

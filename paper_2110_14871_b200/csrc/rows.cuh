@@ -13,6 +13,8 @@ gdws_status_t check_rows8(const char *call, const char *name, const gdws_rows8_t
 gdws_status_t check_pointwise8(const gdws_rows8_t *x, const gdws_rows8_t *w, const float *bias, const gdws_rows_t *y);
 gdws_status_t rows_device(int *device, int *sms);       // the current device, checked to be compute capability 10.x, and its SMs
 
+cudaError_t rows_status_word(int **word);               // where the calls on rows of the current device note a wait that ran out
+
 // A launch's result as a status; a refused launch leaves no error behind for the caller's next CUDA call.
 inline gdws_status_t launched(cudaError_t e, const char *what)
 {

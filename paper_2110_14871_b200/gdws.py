@@ -35,7 +35,7 @@ EXPORTS = [
     "gdws_last_error", "gdws_version", "gdws_destroy", "gdws_forward_static", "gdws_static_scratch_bytes",
     "gdws_measure_fma_rate", "gdws_measure_code_size", "gdws_selftest_wait", "gdws_plan_gdw_stage", "gdws_plan_form",
     "gdws_plan_kernel", "gdws_quantize_rows", "gdws_norm_quantize_rows", "gdws_dequantize_rows", "gdws_pointwise8",
-    "gdws_pointwise8_kernel", "gdws_rows_status",
+    "gdws_pointwise8_kernel", "gdws_rows_status", "gdws_rows_selftest_wait",
 ]
 
 
@@ -139,6 +139,8 @@ def lib() -> ctypes.CDLL:
     L.gdws_pointwise8_kernel.restype = ci
     L.gdws_rows_status.argtypes = []
     L.gdws_rows_status.restype = ci
+    L.gdws_rows_selftest_wait.argtypes = [ctypes.c_uint, vp]
+    L.gdws_rows_selftest_wait.restype = ci
     L.gdws_last_error.argtypes = []
     L.gdws_last_error.restype = ctypes.c_char_p
     L.gdws_version.argtypes = []
@@ -535,6 +537,11 @@ def pointwise8_kernel(q, scale, w, w_scale, y) -> int:
     px, pw, py = _steps(d.rows8[0], q, scale, "q", device), _steps(d.rows8[1], w, w_scale, "w", device), _values(d.rows[0], y, "y", device)
     _check(lib().gdws_pointwise8_kernel(px, pw, py, ctypes.byref(kernel)))
     return kernel.value
+
+
+def rows_selftest_wait(polls: int = 64, stream=None) -> None:
+    """gdws_rows_selftest_wait: a bounded wait that runs out; the next rows_status() raises GDWS_ERR_DEVICE_TIMEOUT once."""
+    _check(lib().gdws_rows_selftest_wait(polls, _stream(stream)))
 
 
 def rows_status() -> None:
