@@ -321,12 +321,11 @@ GDWS_API size_t gdws_static_scratch_bytes(void);
  * threads at once are independent.  Buffers are those of the current device.
  *
  * Element (r, c) of gdws_rows_t is ptr[r * ld + c], of gdws_rows8_t it stands for scale[r] * q[r * ld + c].  rows >= 0 (at most
- * 2^31 - 1024; with 0 rows nothing is done and pointers may be NULL), 1 <= cols <= 2^30, ld >= cols (not looked at for a single row),
- * (rows - 1) * ld <= 2^56.
- * Pointers need the alignment of their element type only, whatever the general rule says.  Nothing but the elements themselves is
- * written, and used: neither what lies between cols and ld nor rows behind the last one (an aligned 16-byte piece that holds an
- * element may be read as a whole).  Outputs must not overlap inputs or each
- * other except where noted; columns of one buffer that do not meet (same ld) are no overlap.
+ * 2^31 - 1024; with 0 rows nothing is done and pointers may be NULL), 1 <= cols <= 2^30, ld >= cols and (rows - 1) * ld <= 2^56 (ld is
+ * not looked at for a single row).  Pointers need the alignment of their element type only, whatever the general rule says.  Nothing
+ * but the elements themselves is written, and used: neither what lies between cols and ld nor rows behind the last one, whatever
+ * it holds (an aligned 16-byte piece that holds an element may be read as a whole).  Outputs must not overlap inputs or each other
+ * except where noted; columns of one buffer that do not meet (same ld) are no overlap.
  */
 typedef struct {
     void *ptr; /* DEVICE */
@@ -359,7 +358,8 @@ GDWS_API gdws_status_t gdws_quantize_rows(const gdws_rows_t *x, const gdws_rows8
  *   residual   NULL: none;  total   NULL: not written.  Type, rows and cols of x.  total may be the very rows of x or of residual
  *   weight     DEVICE, cols entries of weight_dtype (F32 or BF16), NULL: ones
  *   eps        finite, at least 2^-126
- * Sums are fp32, those of long rows partly in 64 bits.  A row with an infinity or NaN in x, residual, h * weight or the sum of squares gets scale NaN and zeros.
+ * Sums are fp32, those of long rows partly in 64 bits.  A row with an infinity or NaN in x, residual, h * weight or the sum of
+ * squares gets scale NaN and zeros.
  * Errors: as gdws_quantize_rows.
  */
 GDWS_API gdws_status_t gdws_norm_quantize_rows(const gdws_rows_t *x, const gdws_rows_t *residual, const gdws_rows_t *total,

@@ -685,8 +685,8 @@ int slices_stages(const P8Choice &c, int pieces)
     return mine <= most ? mine : most / kP8Loaders * kP8Loaders;
 }
 
-
-// Estimated times in us, of calls on data in L2, fitted to 250 timings of 40 sizes on a B200 (most within 15 %).
+// Estimated times in us, of calls on data in L2, fitted by hand to timings of 40 sizes with each kernel on a B200 (most within 15 %;
+// they decide between kernels, nothing else rests on them).
 //
 // Few rows: reading w at what the dot products of so many rows leave of it, and the sums across a warp.
 double few_us(const P8Params &P)

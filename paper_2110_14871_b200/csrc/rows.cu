@@ -162,7 +162,7 @@ union Raw {
 // c may be negative.  whole: all of them exist and lie on a boundary of 16 bytes.  Others are taken one by one, or, where they are
 // known to lie on such a boundary (ALIGNED), as every piece that holds a value of the row, and what else it holds is set to zero.
 // (1000 x 10001, quantization: 21 us one by one, 13.5 by pieces.  Norms of rows on boundaries, whose only such vector is the last, were
-// slower by pieces: 8192 x 4096 46 -> 60 us, whatever the order of the conditions.)
+// slower by pieces: 8192 x 4096, in an earlier form, 46 -> 60 us, whatever the order of the conditions.)
 template <int VEC, bool ALIGNED, typename T>
 __device__ __forceinline__ void load_raw(const T *row, int c, int cols, bool whole, Raw<VEC, T> &b)
 {
@@ -586,7 +586,7 @@ cudaError_t launch_rows(const RowsParams &P, cudaStream_t st)
     return launch_overlapped(rows8_kernel<T, VEC, SHIFTED, N, TPR, NORM>, dim3((unsigned)(((int64_t)P.rows + per - 1) / per)), TPR < 128 ? 128u : (unsigned)TPR, 0, st, P);
 }
 // Values and threads for a row.  With many rows few threads with many values each: loads in flight, and what a row costs every
-// thread (sums, divisions) spread over them (8192 x 4096 bf16, norm: 128 threads 45.3 us, 256 47.3, 512 78).  With few rows, where
+// thread (sums, divisions) spread over them (8192 x 4096 bf16, an earlier form of the norm: 128 threads 45.3 us, 256 47.3, 512 78).  With few rows, where
 // the chip is not full anyway, more threads.
 template <typename T, bool SHIFTED, bool NORM>
 cudaError_t launch_rows(const RowsParams &P, bool few, cudaStream_t st)
@@ -602,27 +602,28 @@ cudaError_t launch_rows(const RowsParams &P, bool few, cudaStream_t st)
     if (n <= 128) return launch_rows<T, 8, SHIFTED, 16, 8, NORM>(P, st);
     if (n <= 256) return launch_rows<T, 8, SHIFTED, 16, 16, NORM>(P, st);
     if (n <= 512) return launch_rows<T, 8, SHIFTED, 16, 32, NORM>(P, st);
-    if constexpr (NORM && SHIFTED) {       // more registers a value: fewer values where that is not half of the threads more (10000 x 801 bf16 31.8 -> 24.5 us)
+    // (Norms below: contiguous rows, with residual, total and fp32 weight; without the rule -> with it.)
+    if constexpr (NORM && SHIFTED) {       // more registers a value: fewer values where that is not half of the threads more (10000 x 801 bf16 36.2 -> 24.7 us, 4000 x 3001 48 -> 37.5)
         if (n > 768 && n <= 1024) return launch_rows<T, 8, SHIFTED, 16, 64, NORM>(P, st);
         if (n > 1536 && n <= 2048) return launch_rows<T, 8, SHIFTED, 16, 128, NORM>(P, st);
         if (n > 2048 && n <= 4096) return launch_rows<T, 8, SHIFTED, 16, 256, NORM>(P, st);
     }
     if (n <= 768) return launch_rows<T, 8, SHIFTED, 24, 32, NORM>(P, st);
     if (n <= 1024) return launch_rows<T, 8, SHIFTED, 32, 32, NORM>(P, st);
-    if constexpr (!NORM && !SHIFTED && sizeof(T) == 2) {       // few registers: a warp to a row goes further (16384 x 1280 13.7 -> 12.0 us)
+    if constexpr (!NORM && !SHIFTED && sizeof(T) == 2) {       // few registers: a warp to a row goes further (16384 x 1152 13.3 -> 11.9 us; with 48 values up to 1536 13.2 -> 13.1)
         if (n <= 1280) return launch_rows<T, 8, SHIFTED, 40, 32, NORM>(P, st);
     }
     if (n <= 1536) return launch_rows<T, 8, SHIFTED, 24, 64, NORM>(P, st);
     if (n <= 2048) return launch_rows<T, 8, SHIFTED, 32, 64, NORM>(P, st);
     if (n <= 4096) return launch_rows<T, 8, SHIFTED, 32, 128, NORM>(P, st);
-    if constexpr (NORM && (SHIFTED || sizeof(T) == 4)) {       // more registers a value: fewer values (4000 x 7999 bf16 79 -> 69 us, 2000 x 7000 fp32 42 -> 36)
+    if constexpr (NORM && (SHIFTED || sizeof(T) == 4)) {       // more registers a value: fewer values (4000 x 7999 bf16 131 -> 82 us, 2000 x 7000 fp32 42 -> 36)
         if (SHIFTED && n <= 6144) return launch_rows<T, 8, SHIFTED, 24, 256, NORM>(P, st);
         if (n <= 8192) return launch_rows<T, 8, SHIFTED, 16, 512, NORM>(P, st);
     }
     if (n <= 6144) return launch_rows<T, 8, SHIFTED, 24, 256, NORM>(P, st);
     if (n <= 8192) return launch_rows<T, 8, SHIFTED, 32, 256, NORM>(P, st);
     if (n <= 12288) return launch_rows<T, 8, SHIFTED, 24, 512, NORM>(P, st);
-    if constexpr (NORM) {        // 32 values and what is added to them leave one block of 512 threads on an SM (2000 x 16000 bf16 64 -> 56 us)
+    if constexpr (NORM) {        // 32 values and what is added to them leave one block of 512 threads on an SM (2000 x 16000 bf16 63 -> 56 us)
         if (n <= 16384) return launch_rows<T, 8, SHIFTED, 16, 1024, NORM>(P, st);
     }
     if (n <= 16384) return launch_rows<T, 8, SHIFTED, 32, 512, NORM>(P, st);

@@ -23,8 +23,10 @@ inline gdws_status_t launched(cudaError_t e, const char *what)
     return cuda_fail(e, what);
 }
 
-// An arrival, at a barrier of either block of a pair, that publishes nothing in memory: the tensor memory it gives back has been
-// read into registers.  (A releasing arrival waits until the warp's stores to y have been performed.)
+// An arrival, at a barrier of either block of a pair, that gives tensor memory back.  It publishes nothing in memory and orders nothing by
+// itself: the caller has waited for its loads from tensor memory (tcgen05.wait::ld) and fenced them before the threads' meeting
+// (tcgen05.fence::before_thread_sync), so the registers hold what is about to be overwritten.  (A releasing arrival also waits until
+// the warp's stores to y have been performed.)
 __device__ __forceinline__ void mbar_arrive_relaxed(uint32_t bar)
 {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
