@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import re
 import struct
 import threading
 from typing import Optional, Sequence, Tuple
@@ -400,7 +401,7 @@ def _rows_setup():
     if not os.path.exists(os.path.join(_HERE, "_rows.so")):
         raise FileNotFoundError("_rows.so is missing: build it with `python -m paper_2110_14871_b200.build`")
     from . import _rows as native
-    if native.torch_version != torch.__version__.split("+")[0]:
+    if re.match(r"[\d.]*\d", native.torch_version)[0] != re.match(r"[\d.]*\d", torch.__version__)[0]:      # a pre-release's header leaves its suffix out
         raise ImportError(f"_rows.so was built against torch {native.torch_version}, this is {torch.__version__}: build it anew with `python -m paper_2110_14871_b200.build`")
     if not torch.cuda.is_available():
         _get_device = lambda: -1  # noqa: E731

@@ -42,3 +42,10 @@ def test_a_binding_for_another_torch_is_not_loaded(monkeypatch):
     q = torch.zeros((4, 8), dtype=torch.int8)
     with pytest.raises(ImportError, match="1.0.0"):
         gdws.quantize_rows(torch.zeros((4, 8)), q, torch.zeros(4))
+
+
+def test_a_pre_release_of_the_same_torch_is(monkeypatch):
+    """Its version has a suffix that its headers leave out."""
+    monkeypatch.setattr(torch, "__version__", torch.__version__.split("+")[0] + "a0+git1234567")
+    monkeypatch.setattr(gdws, "_rows", None)
+    assert gdws._rows_setup() is not None
