@@ -5,7 +5,7 @@ import torch
 from paper_2110_14871_b200 import build as gbuild
 from paper_2110_14871_b200 import gdws
 
-from rows8_util import Field, steps_of
+from rows8_util import Field, product_of, steps_of
 from test_gpu_rows8 import TYPES, norm_bound, values
 
 pytestmark = pytest.mark.gpu
@@ -67,3 +67,27 @@ def test_norms_of_wide_rows(rows, cols, gap, shift, dtype, operands):
     for f in (x, r, total, q, scale):
         if f:
             f.check("a matrix")
+
+
+def test_streams_given_to_the_calls():
+    """stream=: an object or a handle; the work is ordered there, behind what fills its inputs late."""
+    w, w_scale = gdws.empty_rows8(72, 1000)
+    gdws.quantize_rows(values(72, 1000, "f32", 3), w, w_scale)
+    late, gain = values(400, 1000, "bf16", 4), torch.nn.Parameter(torch.ones(1000, device="cuda"))
+    for given in (lambda s: s, lambda s: s.cuda_stream):
+        s = torch.cuda.Stream()
+        x, r = torch.zeros((400, 1000), dtype=torch.bfloat16, device="cuda"), values(400, 1000, "bf16", 5)
+        q, scale = gdws.empty_rows8(400, 1000)
+        total, y, z = torch.empty_like(x), torch.empty_like(x), torch.empty((400, 72), device="cuda")
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(2_000_000)                # about a millisecond
+            x.copy_(late)
+        gdws.norm_quantize_rows(x, q, scale, weight=gain, residual=r, total=total, stream=given(s))
+        gdws.dequantize_rows(q, scale, y, stream=given(s))
+        gdws.pointwise8(q, scale, w, w_scale, z, stream=given(s))
+        torch.cuda.current_stream().wait_stream(s)
+        h = late.float() + r.float()
+        assert torch.equal(q, steps_of(h)[0]) and torch.equal(total, h.bfloat16()) and torch.equal(y, (q.float() * scale[:, None]).bfloat16())
+        want, bound = product_of(q, scale, w, w_scale, None, False)
+        assert ((z.double() - want).abs() <= bound).all()
